@@ -141,12 +141,44 @@ typedef struct {
   const int32_t *cu_step_lens_host;  /* host   [batch + 1] */
 } arb_batch;
 
+/* The 8-bit cache.  A row (the key or the value of one position and kv head, head_dim elements) is held as e4m3 elements
+ * (the OCP format: 4 exponent and 3 mantissa bits, largest 448) and one power-of-two scale: with e the least integer for
+ * which max|x| <= 448 * 2^e, but at least -100, element = e4m3(x * 2^-e), rounded to nearest even, and the scale byte is
+ * e + 127; the row stands for element * 2^e, which bf16 holds exactly.  2 * head_dim + 2 bytes a position and kv head
+ * against 4 * head_dim.  Keys are rounded once, from the fp32 rotated values.
+ * A position whose key or value row holds a NaN, an infinity or a magnitude of 2^120 or more is stored as a key of NaNs
+ * and a value of zeros (scale bytes 127): rows that attend to it get NaN, rows that do not see it are not affected.
+ * k_pool / v_pool: HOST arrays of n_layers DEVICE pointers to uint8 [n_blocks, Hkv, kv_block, head_dim]; k_scale / v_scale:
+ * HOST arrays of n_layers DEVICE pointers to uint8 [n_blocks, Hkv, kv_block].  Blocks and tables are those of arb_kv.  Pools and scales
+ * are aligned to 16 bytes.  Slots that were never written may hold anything. */
+typedef struct {
+  void *const *k_pool, *const *v_pool;
+  uint8_t *const *k_scale, *const *v_scale;
+  int32_t n_blocks;
+} arb_kv8;
+
+/* One layer of a cache, DEVICE pointers: bf16 pools with k_scale and v_scale NULL, or 8-bit pools with both scales. */
+typedef struct {
+  void *k_pool, *v_pool;
+  uint8_t *k_scale, *v_scale;
+} arb_kv_layer;
+
 typedef struct arb_model arb_model;
 
 /* Validates the shape and copies the configuration and pointer tables (host
  * memory only).  *out is owned by the caller until arb_model_destroy. */
 arb_status arb_model_create(const arb_model_cfg *cfg, const arb_weights *w, arb_model **out);
 arb_status arb_model_destroy(arb_model *m);
+
+/* Gains of an RMS norm over head_dim that every query head (g_q) and every key head (g_k) of a layer goes through before the
+ * rotary embedding: u <- u * g / sqrt(mean(u^2) + rms_eps).  HOST arrays of n_layers DEVICE pointers to fp32 [head_dim], aligned
+ * to 16 bytes; copied (the pointers; the gains must outlive the model).  Both NULL: no head norms (the default). */
+arb_status arb_model_set_head_norms(arb_model *m, const float *const *g_q, const float *const *g_k);
+
+/* Caps the attention scores of every layer: the logit x = q.k / sqrt(head_dim) becomes cap * tanh(x / cap).  0: no cap (the
+ * default); otherwise 0.01 <= softcap <= 1024 (ARB_EUNSUPPORTED; beyond, fp32 would not hold the capped logit to the accuracy of its
+ * probability).  Like the head norms it applies to the calls made after it. */
+arb_status arb_model_set_softcap(arb_model *m, float softcap);
 
 /* Bytes of device workspace the hot calls need for batches of at most
  * max_total_tokens step tokens in at most max_batch sequences whose context
@@ -184,6 +216,23 @@ arb_status arb_score_steps_noalloc(arb_model *m, const arb_kv *kv, const arb_bat
  * prefill).  No head.  hidden_out as above, may be NULL. */
 arb_status arb_prefill(arb_model *m, const arb_kv *kv, const arb_batch *batch, void *hidden_out, void *ws,
                        size_t ws_bytes, void *stream);
+
+/* arb_score_steps and arb_prefill on an 8-bit cache; everything else as there, the workspace included. */
+arb_status arb_score_steps_kv8(arb_model *m, const arb_kv8 *kv, const arb_batch *batch, float tau, float *scores,
+                               uint8_t *escalate, void *hidden_out, void *ws, size_t ws_bytes, void *stream);
+arb_status arb_prefill_kv8(arb_model *m, const arb_kv8 *kv, const arb_batch *batch, void *hidden_out, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* Converts n_blocks cache blocks of one layer: arb_kv8_pack from bf16 pools (src, scales NULL) into 8-bit pools (dst),
+ * arb_kv8_unpack from 8-bit pools (src) into bf16 pools (dst), exactly.  Block src_blocks[i] of src goes to block dst_blocks[i] of
+ * dst, i < n_blocks; device int32 [n_blocks], either may be NULL (block i).  All kv_block rows of a block are converted, those beyond a
+ * sequence's length with whatever they hold.  Block ids are trusted; a source block may be listed more than once, a destination block
+ * must not be (which of its sources it then holds, row by row, is undefined).  src and dst do not overlap.  head_dim 64 or 128.
+ * The blocks listed are converted whatever the pools' other blocks hold; those stay as they are.  n_blocks == 0 is a no-op. */
+arb_status arb_kv8_pack(const arb_kv_layer *src, const int32_t *src_blocks, const arb_kv_layer *dst, const int32_t *dst_blocks,
+                        int32_t n_blocks, int32_t n_kv_heads, int32_t head_dim, void *stream);
+arb_status arb_kv8_unpack(const arb_kv_layer *src, const int32_t *src_blocks, const arb_kv_layer *dst, const int32_t *dst_blocks,
+                          int32_t n_blocks, int32_t n_kv_heads, int32_t head_dim, void *stream);
 
 /* The decision alone (Fig. 1; Alg. 1; Section 3.1 for the RSD sense), so that
  * tau can be swept without repeating the forward.  Also serves the oracle
@@ -317,6 +366,12 @@ arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_
                                const void *k_pool, const void *v_pool, const arb_batch *batch, void *out, void *ws,
                                size_t ws_bytes, void *stream);
 
+/* Append-attention of one layer over a cache of either type, with softcap as in arb_model_set_softcap (the argument counts, not the
+ * model's).  The other arguments are those of arb_stage_attention, of which this is the general form. */
+arb_status arb_stage_attention_kv(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
+                                  const arb_kv_layer *kv, float softcap, const arb_batch *batch, void *out, void *ws,
+                                  size_t ws_bytes, void *stream);
+
 /* RMSNorm rows: x fp32 [T, d] -> out bf16 [T, d] = x / sqrt(mean(x^2) + eps) * g. */
 arb_status arb_stage_rmsnorm(const float *x, const float *g, float eps, int32_t T, int32_t d, void *out, void *stream);
 
@@ -324,6 +379,14 @@ arb_status arb_stage_rmsnorm(const float *x, const float *g, float eps, int32_t 
  * positions prefix_lens[b] + i, and the K/V append into one layer's pool. */
 arb_status arb_stage_rope_append(const arb_model *m, void *qkv, void *k_pool, void *v_pool, const arb_batch *batch,
                                  void *ws, size_t ws_bytes, void *stream);
+
+/* Head norms, rotary embedding and cache append of one layer in one launch: the q and k heads of qkv (bf16 [T, (Hq+2Hkv)*hd])
+ * are normed as in arb_model_set_head_norms (g_q, g_k: device fp32 [hd] or NULL, each for itself: not normed; the model's own gains do not
+ * count), rotated at positions prefix_lens[b] + i, and k and v stored in the layer's pools of either type.  The queries go to q_out
+ * (bf16 [T, Hq*hd], not overlapping qkv), or in place with q_out NULL; with q_scaled they carry the factor
+ * log2(e) / sqrt(hd), as arb_stage_attention takes them.  Needs no workspace. */
+arb_status arb_stage_norm_rope_append(const arb_model *m, void *qkv, const float *g_q, const float *g_k, int32_t q_scaled,
+                                      const arb_kv_layer *kv, const arb_batch *batch, void *q_out, void *stream);
 
 /* Final RMSNorm of the residual stream h (fp32 [T, d]) followed by pooling, head and threshold
  * (Section 4.2; Alg. 1): hidden_out bf16 [T, d] or NULL; scores fp32 [batch]; escalate uint8 [batch] or
@@ -341,6 +404,11 @@ arb_status arb_stage_norm_pool_head(const float *h, const float *g_final, float 
 arb_status arb_stage_layers(arb_model *m, const arb_kv *kv, const arb_batch *batch, int32_t layer_begin,
                             int32_t layer_end, const float *h_in, float *h_out, void *ws, size_t ws_bytes,
                             void *stream);
+
+/* The same on an 8-bit cache. */
+arb_status arb_stage_layers_kv8(arb_model *m, const arb_kv8 *kv, const arb_batch *batch, int32_t layer_begin,
+                                int32_t layer_end, const float *h_in, float *h_out, void *ws, size_t ws_bytes,
+                                void *stream);
 
 /* Timing hook for measurement harnesses (no paper passage: it computes nothing).
  * While armed, arb_score_steps / arb_prefill record start[i] before and stop[i]

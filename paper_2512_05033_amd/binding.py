@@ -6,6 +6,7 @@ shared library is missing, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -29,7 +30,8 @@ NOALLOC_SCRATCH_BYTES = 64 << 20      # ARB_NOALLOC_SCRATCH_BYTES of include/arb
 
 EXPORTS = ["arb_model_create", "arb_model_destroy", "arb_workspace_bytes", "arb_score_steps", "arb_score_steps_noalloc", "arb_prefill",
            "arb_route", "arb_next_token", "arb_next_token_workspace_bytes", "arb_first_stop", "arb_step_advance", "arb_pack_steps", "arb_advantage_route", "arb_budget_threshold", "arb_slot_mapping", "arb_stage_gemm", "arb_pack_k_blocked", "arb_w4_quantize", "arb_w3_quantize", "arb_stage_gemm_w4", "arb_stage_attention", "arb_stage_rmsnorm",
-           "arb_stage_rope_append", "arb_stage_norm_pool_head", "arb_stage_layers", "arb_gemm_large_tile_columns", "arb_model_trace", "arb_model_trace_count",
+           "arb_stage_rope_append", "arb_stage_norm_pool_head", "arb_stage_layers", "arb_model_set_head_norms", "arb_model_set_softcap", "arb_score_steps_kv8",
+           "arb_prefill_kv8", "arb_stage_layers_kv8", "arb_kv8_pack", "arb_kv8_unpack", "arb_stage_attention_kv", "arb_stage_norm_rope_append", "arb_gemm_large_tile_columns", "arb_model_trace", "arb_model_trace_count",
            "arb_last_error"]
 
 
@@ -56,6 +58,15 @@ class _Weights(C.Structure):
 
 class _KV(C.Structure):
     _fields_ = [("k_pool", C.POINTER(C.c_void_p)), ("v_pool", C.POINTER(C.c_void_p)), ("n_blocks", C.c_int32)]
+
+
+class _KV8(C.Structure):
+    _fields_ = [("k_pool", C.POINTER(C.c_void_p)), ("v_pool", C.POINTER(C.c_void_p)), ("k_scale", C.POINTER(C.c_void_p)),
+                ("v_scale", C.POINTER(C.c_void_p)), ("n_blocks", C.c_int32)]
+
+
+class _KVLayer(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
 class _Batch(C.Structure):
@@ -116,6 +127,18 @@ def load_library(path: Optional[str] = None):
                                              C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.arb_stage_layers.argtypes = [C.c_void_p, C.POINTER(_KV), C.POINTER(_Batch), C.c_int32, C.c_int32, C.c_void_p,
                                      C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.arb_model_set_head_norms.argtypes = [C.c_void_p, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p)]
+    lib.arb_model_set_softcap.argtypes = [C.c_void_p, C.c_float]
+    lib.arb_score_steps_kv8.argtypes = [C.c_void_p, C.POINTER(_KV8), *lib.arb_score_steps.argtypes[2:]]
+    lib.arb_prefill_kv8.argtypes = [C.c_void_p, C.POINTER(_KV8), *lib.arb_prefill.argtypes[2:]]
+    lib.arb_stage_layers_kv8.argtypes = [C.c_void_p, C.POINTER(_KV8), *lib.arb_stage_layers.argtypes[2:]]
+    for convert in (lib.arb_kv8_pack, lib.arb_kv8_unpack):
+        convert.argtypes = [C.POINTER(_KVLayer), C.c_void_p, C.POINTER(_KVLayer), C.c_void_p, C.c_int32, C.c_int32,
+                            C.c_int32, C.c_void_p]
+    lib.arb_stage_attention_kv.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.POINTER(_KVLayer), C.c_float,
+                                           C.POINTER(_Batch), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.arb_stage_norm_rope_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(_KVLayer),
+                                               C.POINTER(_Batch), C.c_void_p, C.c_void_p]
     lib.arb_model_trace.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int32]
     lib.arb_model_trace_count.argtypes = [C.c_void_p]
     lib.arb_model_trace_count.restype = C.c_int32
@@ -160,8 +183,10 @@ class Model:
 
     def __init__(self, *, n_layers, d_model, n_q_heads, n_kv_heads, head_dim, d_ffn, vocab, weights,
                  rms_eps=1e-6, rope_base=10000.0, kv_block=16, pool=ARB_POOL_MEAN, has_router_head=True,
-                 block_gate_up=True):
-        """block_gate_up: also hand the library K-blocked copies of the gate/up weights (arb_pack_k_blocked; made
+                 block_gate_up=True, head_norms=None, softcap=0.0):
+        """head_norms: (gains of the query heads, gains of the key heads), two lists of fp32 [head_dim] tensors, one per
+        layer (arb_model_set_head_norms); softcap: cap of the attention scores, 0 for none (arb_model_set_softcap).
+        block_gate_up: also hand the library K-blocked copies of the gate/up weights (arb_pack_k_blocked; made
         here on the weights' device, 4 F d bytes per layer); bf16 weights only."""
         lib = load_library()
         w = weights
@@ -196,6 +221,19 @@ class Model:
         _check(lib.arb_model_create(C.byref(self.cfg), C.byref(cw), C.byref(self.handle)))
         self.weights = w
         self.device = w.embed.device
+        try:
+            if head_norms is not None:
+                for gains in head_norms:
+                    if len(gains) != n_layers or any(tuple(g.shape) != (head_dim,) for g in gains):
+                        raise ValueError(f"head_norms: {n_layers} gains of [{head_dim}] each for the queries and for the keys")
+                self._keep += [_dev(g, f32) for gains in head_norms for g in gains]
+                g_q, g_k = (_ptr_array(gains) for gains in head_norms)
+                _check(lib.arb_model_set_head_norms(self.handle, g_q, g_k))
+            if softcap:
+                _check(lib.arb_model_set_softcap(self.handle, float(softcap)))
+        except Exception:
+            self.close()
+            raise
 
     def workspace_bytes(self, max_batch: int, max_total_tokens: int, max_ctx: int) -> int:
         return int(load_library().arb_workspace_bytes(self.handle, max_batch, max_total_tokens, max_ctx))
@@ -220,6 +258,45 @@ class KVCache:
         self.v_pools = [_dev(t, torch.bfloat16) for t in v_pools]
         self._k, self._v = _ptr_array(self.k_pools), _ptr_array(self.v_pools)
         self.c = _KV(self._k, self._v, int(k_pools[0].shape[0]))
+
+
+class KVLayer:
+    """One layer of a cache: bf16 pools [n_blocks, Hkv, kv_block, head_dim], or float8_e4m3fn pools (8-bit) with the scale
+    bytes of their rows, uint8 [n_blocks, Hkv, kv_block]."""
+
+    def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        if (k_scale is None) != (v_scale is None):
+            raise ValueError("scales of the keys and of the values, or neither")
+        self.kv8 = k_scale is not None
+        for t in (k_pool, v_pool):
+            _dev(t, torch.float8_e4m3fn if self.kv8 else torch.bfloat16)
+        if k_pool.dim() != 4 or k_pool.shape != v_pool.shape or k_pool.shape[2] != 16:
+            raise ValueError(f"pools are [n_blocks, Hkv, 16, head_dim], got {tuple(k_pool.shape)} and {tuple(v_pool.shape)}")
+        for t in (k_scale, v_scale) if self.kv8 else ():
+            if _dev(t, torch.uint8).shape != k_pool.shape[:3]:
+                raise ValueError(f"scales are {tuple(k_pool.shape[:3])}, got {tuple(t.shape)}")
+        self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
+        self.c = _KVLayer(_ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale))
+
+
+class KVCache8:
+    """Per-layer 8-bit pools (KVLayer with scales).  arb_prefill, arb_score_steps and arb_stage_layers take it in the place
+    of a KVCache."""
+
+    def __init__(self, layers: List[KVLayer]):
+        if not layers or not all(l.kv8 for l in layers) or len({l.k_pool.shape for l in layers}) != 1:
+            raise ValueError("an 8-bit cache is a list of 8-bit layers of one shape")
+        self.layers = list(layers)
+        self._tables = [_ptr_array([getattr(l, n) for l in self.layers]) for n in ("k_pool", "v_pool", "k_scale", "v_scale")]
+        self.c = _KV8(*self._tables, int(layers[0].k_pool.shape[0]))
+
+    @classmethod
+    def empty(cls, n_layers: int, n_blocks: int, n_kv_heads: int, head_dim: int, device="cuda") -> "KVCache8":
+        """A new cache whose slots hold zeros."""
+        pool = lambda: torch.zeros(n_blocks, n_kv_heads, 16, head_dim, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        scale = lambda: torch.full((n_blocks, n_kv_heads, 16), 127, dtype=torch.uint8, device=device)
+        return cls([KVLayer(pool(), pool(), scale(), scale()) for _ in range(n_layers)])
 
 
 class DeviceBatch:
@@ -256,6 +333,25 @@ def _workspace(model: Model, batch: DeviceBatch, ws: Optional[torch.Tensor]) -> 
     return ws
 
 
+def _by_cache(kv, name: str):
+    """The library's entry for this type of cache."""
+    return getattr(load_library(), name + ("_kv8" if isinstance(kv, KVCache8) else ""))
+
+
+def _on(stream):
+    """Where outputs and scratch of a call are allocated: on the stream that the call runs on, so that neither memory still in
+    use there is handed out nor this memory is handed on before the call has run."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _here(*tensors):
+    """The library works on the current device; tensors elsewhere are refused."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
 def arb_score_steps(model: Model, kv: KVCache, batch: DeviceBatch, tau: float, *, want_hidden: bool = False,
                     ws: Optional[torch.Tensor] = None, scores=None, escalate=None, hidden=None, stream=None):
     """-> (scores fp32 [B] or None, escalate uint8 [B] or None, hidden bf16 [T, d] or None)."""
@@ -268,15 +364,17 @@ def arb_score_steps(model: Model, kv: KVCache, batch: DeviceBatch, tau: float, *
     if want_hidden and hidden is None:
         hidden = torch.empty(batch.total_tokens, model.cfg.d_model, dtype=torch.bfloat16, device=dev)
     ws = _workspace(model, batch, ws)
-    _check(load_library().arb_score_steps(model.handle, C.byref(kv.c), C.byref(batch.c), float(tau), _ptr(scores),
-                                          _ptr(escalate), _ptr(hidden), ws.data_ptr(), ws.numel(), _stream(stream)))
+    _check(_by_cache(kv, "arb_score_steps")(model.handle, C.byref(kv.c), C.byref(batch.c), float(tau), _ptr(scores),
+                                            _ptr(escalate), _ptr(hidden), ws.data_ptr(), ws.numel(), _stream(stream)))
     return scores, escalate, hidden
 
 
 def arb_score_steps_noalloc(model: Model, kv: KVCache, batch: DeviceBatch, tau: float, *, scores=None, escalate=None,
                             hidden=None, stream=None):
-    """arb_score_steps on the library's static scratch buffer.  The caller passes every output tensor
+    """arb_score_steps on the library's static scratch buffer (bf16 caches only).  The caller passes every output tensor
     (scores and escalate when the model has a head; hidden optional); nothing is allocated here."""
+    if isinstance(kv, KVCache8):
+        raise ValueError("arb_score_steps_noalloc takes a bf16 cache; use arb_score_steps")
     _check(load_library().arb_score_steps_noalloc(model.handle, C.byref(kv.c), C.byref(batch.c), float(tau),
                                                   _ptr(scores), _ptr(escalate), _ptr(hidden), _stream(stream)))
     return scores, escalate, hidden
@@ -288,8 +386,8 @@ def arb_prefill(model: Model, kv: KVCache, batch: DeviceBatch, *, want_hidden: b
     if want_hidden:
         hidden = torch.empty(batch.total_tokens, model.cfg.d_model, dtype=torch.bfloat16, device=model.device)
     ws = _workspace(model, batch, ws)
-    _check(load_library().arb_prefill(model.handle, C.byref(kv.c), C.byref(batch.c), _ptr(hidden), ws.data_ptr(),
-                                      ws.numel(), _stream(stream)))
+    _check(_by_cache(kv, "arb_prefill")(model.handle, C.byref(kv.c), C.byref(batch.c), _ptr(hidden), ws.data_ptr(),
+                                        ws.numel(), _stream(stream)))
     return hidden
 
 
@@ -507,6 +605,86 @@ def arb_stage_rope_append(model: Model, qkv: torch.Tensor, k_pool: torch.Tensor,
                                                 ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
+def _check_layer(model: Model, kv: KVLayer):
+    if kv.k_pool.shape[1] != model.cfg.n_kv_heads or kv.k_pool.shape[3] != model.cfg.head_dim:
+        raise ValueError(f"pools of shape {tuple(kv.k_pool.shape)} for {model.cfg.n_kv_heads} kv heads of {model.cfg.head_dim}")
+
+
+def arb_stage_attention_kv(model: Model, q: torch.Tensor, kv: KVLayer, batch: DeviceBatch, softcap: float = 0.0,
+                           ws: Optional[torch.Tensor] = None, stream=None, q_scaled: bool = False,
+                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """arb_stage_attention over one layer of either type of cache, scores capped by softcap * tanh(x / softcap) if softcap > 0.
+    q bf16 [T, row] whose first Hq*hd columns are the (rotated) query heads -> bf16 [T, Hq*hd]."""
+    T, width = batch.total_tokens, model.cfg.n_q_heads * model.cfg.head_dim
+    _check_layer(model, kv)
+    if _dev(q, torch.bfloat16).dim() != 2 or q.shape[0] < T or q.shape[1] < width:
+        raise ValueError(f"q is bf16 [at least {T}, at least {width}], got {tuple(q.shape)}")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(T, width, dtype=torch.bfloat16, device=q.device)
+        ws = _workspace(model, batch, ws)
+    if _dev(out, torch.bfloat16).numel() < T * width:
+        raise ValueError(f"out holds {out.numel()} elements, need {T * width}")
+    _here(q, kv.k_pool, out, ws, batch.tables)
+    _check(load_library().arb_stage_attention_kv(model.handle, q.data_ptr(), q.shape[1], int(q_scaled), C.byref(kv.c), softcap,
+                                                 C.byref(batch.c), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+def arb_stage_norm_rope_append(model: Model, qkv: torch.Tensor, kv: KVLayer, batch: DeviceBatch, g_q: Optional[torch.Tensor] = None,
+                               g_k: Optional[torch.Tensor] = None, q_scaled: bool = False, out: Optional[torch.Tensor] = None,
+                               in_place: bool = False, stream=None) -> torch.Tensor:
+    """Norms (where a gain, fp32 [hd], is given) and rotates the q and k heads of qkv (bf16 [T, (Hq+2Hkv)*hd]), stores k and v in
+    the layer's pools and returns the queries: bf16 [T, Hq*hd], or qkv itself with in_place."""
+    T, c = batch.total_tokens, model.cfg
+    width = c.n_q_heads * c.head_dim
+    _check_layer(model, kv)
+    if tuple(_dev(qkv, torch.bfloat16).shape) != (T, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim):
+        raise ValueError(f"qkv has shape {tuple(qkv.shape)}")
+    for g in (g_q, g_k):
+        if g is not None and tuple(_dev(g, torch.float32).shape) != (c.head_dim,):
+            raise ValueError(f"a gain has shape {tuple(g.shape)}")
+    if in_place and out is not None:
+        raise ValueError("in_place or out, not both")
+    if out is None and not in_place:
+        with _on(stream):
+            out = torch.empty(T, width, dtype=torch.bfloat16, device=qkv.device)
+    elif out is not None and tuple(_dev(out, torch.bfloat16).shape) != (T, width):
+        raise ValueError(f"out has shape {tuple(out.shape)}")
+    _here(qkv, kv.k_pool, out, g_q, g_k, batch.tables)
+    _check(load_library().arb_stage_norm_rope_append(model.handle, qkv.data_ptr(), _ptr(g_q), _ptr(g_k), int(q_scaled),
+                                                     C.byref(kv.c), C.byref(batch.c), _ptr(out), _stream(stream)))
+    return qkv if in_place else out
+
+
+def _kv8_convert(entry: str, src: KVLayer, dst: KVLayer, src_blocks, dst_blocks, n_blocks, stream):
+    if src.k_pool.shape[1:] != dst.k_pool.shape[1:]:
+        raise ValueError(f"pools of shape {tuple(src.k_pool.shape)} and {tuple(dst.k_pool.shape)}")
+    lists = [b for b in (src_blocks, dst_blocks) if b is not None]
+    if n_blocks is None:
+        n_blocks = lists[0].numel() if lists else src.k_pool.shape[0]
+    for blocks, kv in ((src_blocks, src), (dst_blocks, dst)):
+        room = kv.k_pool.shape[0] if blocks is None else _dev(blocks, torch.int32).numel()
+        if n_blocks > room:
+            raise ValueError(f"{n_blocks} blocks, but a {'pool' if blocks is None else 'list'} of {room}")
+    _here(src.k_pool, dst.k_pool, *lists)
+    _check(getattr(load_library(), entry)(C.byref(src.c), _ptr(src_blocks), C.byref(dst.c), _ptr(dst_blocks), n_blocks,
+                                          src.k_pool.shape[1], src.k_pool.shape[3], _stream(stream)))
+
+
+def arb_kv8_pack(src: KVLayer, dst: KVLayer, src_blocks: Optional[torch.Tensor] = None, dst_blocks: Optional[torch.Tensor] = None,
+                 n_blocks: Optional[int] = None, stream=None) -> None:
+    """bf16 blocks src_blocks[i] of src into the 8-bit blocks dst_blocks[i] of dst (int32 device tensors; None: block i),
+    i < n_blocks (default: the lists' length, or the whole source)."""
+    _kv8_convert("arb_kv8_pack", src, dst, src_blocks, dst_blocks, n_blocks, stream)
+
+
+def arb_kv8_unpack(src: KVLayer, dst: KVLayer, src_blocks: Optional[torch.Tensor] = None, dst_blocks: Optional[torch.Tensor] = None,
+                   n_blocks: Optional[int] = None, stream=None) -> None:
+    """8-bit blocks back into bf16 blocks, exactly; arguments as arb_kv8_pack."""
+    _kv8_convert("arb_kv8_unpack", src, dst, src_blocks, dst_blocks, n_blocks, stream)
+
+
 def arb_stage_norm_pool_head(h: torch.Tensor, g_final: torch.Tensor, eps: float, batch: DeviceBatch,
                              w_head: torch.Tensor, b_head: float, pool: int, tau: float, want_hidden=True, stream=None):
     _dev(h, torch.float32), _dev(g_final, torch.float32), _dev(w_head, torch.float32)
@@ -529,8 +707,8 @@ def arb_stage_layers(model: Model, kv: KVCache, batch: DeviceBatch, layer_begin:
         raise ValueError("residual stream shape")
     h_out = torch.empty_like(h_in)
     ws = _workspace(model, batch, ws)
-    _check(load_library().arb_stage_layers(model.handle, C.byref(kv.c), C.byref(batch.c), layer_begin, layer_end,
-                                           _ptr(h_in), _ptr(h_out), ws.data_ptr(), ws.numel(), _stream(stream)))
+    _check(_by_cache(kv, "arb_stage_layers")(model.handle, C.byref(kv.c), C.byref(batch.c), layer_begin, layer_end,
+                                             _ptr(h_in), _ptr(h_out), ws.data_ptr(), ws.numel(), _stream(stream)))
     return h_out
 
 

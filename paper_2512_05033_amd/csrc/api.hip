@@ -37,6 +37,8 @@ struct arb_model {
   bool w4 = false;
   bool debug_ids = false;                                 // ARB_DEBUG_IDS: range-check ids before every forward
   std::vector<const float *> g_attn, g_mlp;
+  std::vector<const float *> g_q, g_k;                    // gains of the head norms (empty: none)
+  float softcap = 0.f;                                    // cap of the attention scores (0: none)
   const float *g_final, *w_head;
   float b_head;
   int trace_stage = -1, trace_cap = 0, trace_n = 0;      // timing hook (arb_model_trace)
@@ -119,6 +121,41 @@ extern "C" arb_status arb_model_create(const arb_model_cfg *cfg, const arb_weigh
 
 extern "C" arb_status arb_model_destroy(arb_model *m) {
   delete m;
+  return ARB_OK;
+}
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+extern "C" arb_status arb_model_set_head_norms(arb_model *m, const float *const *g_q, const float *const *g_k) {
+  if (!m) return arb_fail(ARB_EINVAL, "null model");
+  if (!g_q != !g_k) return arb_fail(ARB_EINVAL, "arb_model_set_head_norms: gains of the queries and of the keys, or neither");
+  for (int l = 0; g_q && l < m->cfg.n_layers; ++l) {
+    if (!g_q[l] || !g_k[l]) return arb_fail(ARB_EINVAL, "arb_model_set_head_norms: null gain in layer %d", l);
+    if (!aligned16(g_q[l]) || !aligned16(g_k[l])) return arb_fail(ARB_EINVAL, "arb_model_set_head_norms: gain of layer %d is not aligned to 16 bytes", l);
+  }
+  std::vector<const float *> q, k;
+  try {
+    if (g_q) q.assign(g_q, g_q + m->cfg.n_layers);
+    if (g_k) k.assign(g_k, g_k + m->cfg.n_layers);
+  } catch (const std::bad_alloc &) {
+    return arb_fail(ARB_EINVAL, "arb_model_set_head_norms: out of host memory");
+  }
+  m->g_q.swap(q);
+  m->g_k.swap(k);
+  return ARB_OK;
+}
+
+// With a cap c the logit is c tanh(x / c) = c - 2 c / (exp(2 x / c) + 1) in fp32: an error of about 2^-22 c, which has to stay
+// below what bf16 does to the probability (2^-9).
+static arb_status check_softcap(float softcap, const char *name) {
+  if (softcap == 0.f || (softcap >= 0.01f && softcap <= 1024.f)) return ARB_OK;
+  return arb_fail(ARB_EUNSUPPORTED, "%s: softcap %g (0, or 0.01 to 1024)", name, softcap);
+}
+
+extern "C" arb_status arb_model_set_softcap(arb_model *m, float softcap) {
+  if (!m) return arb_fail(ARB_EINVAL, "null model");
+  if (arb_status s = check_softcap(softcap, "arb_model_set_softcap")) return s;
+  m->softcap = softcap;
   return ARB_OK;
 }
 
@@ -239,23 +276,54 @@ static arb_status check_batch(const arb_batch *bt, int kv_block, BatchInfo *info
 
 // ------------------------------------------------------------------------ forward
 
+// The cache of a pass: bf16 pools (no scales), or 8-bit pools.
+struct CacheTables {
+  void *const *k_pool, *const *v_pool;
+  uint8_t *const *k_scale, *const *v_scale;
+  int n_blocks;
+  bool kv8, given;                                         // given: the caller's table of pools was not null
+  arb_kv_layer layer(int l) const { return arb_kv_layer{k_pool[l], v_pool[l], kv8 ? k_scale[l] : nullptr, kv8 ? v_scale[l] : nullptr}; }
+};
+static CacheTables tables_of(const arb_kv *kv) {
+  return kv ? CacheTables{kv->k_pool, kv->v_pool, nullptr, nullptr, kv->n_blocks, false, true} : CacheTables{};
+}
+static CacheTables tables_of(const arb_kv8 *kv) {
+  return kv ? CacheTables{kv->k_pool, kv->v_pool, kv->k_scale, kv->v_scale, kv->n_blocks, true, true} : CacheTables{};
+}
+
+static AttnCache attn_cache(const arb_kv_layer &kv, float softcap) {
+  return AttnCache{kv.k_pool, kv.v_pool, kv.k_scale, kv.v_scale, softcap};
+}
+
+static arb_status check_layer(const arb_kv_layer &kv, const char *name) {
+  if (!kv.k_pool || !kv.v_pool) return arb_fail(ARB_EINVAL, "%s: null kv pool", name);
+  if (!kv.k_scale != !kv.v_scale) return arb_fail(ARB_EINVAL, "%s: scales of the keys and of the values, or neither", name);
+  if (!aligned16(kv.k_pool) || !aligned16(kv.v_pool) || !aligned16(kv.k_scale) || !aligned16(kv.v_scale))
+    return arb_fail(ARB_EINVAL, "%s: a kv pool or its scales are not aligned to 16 bytes", name);
+  return ARB_OK;
+}
+
 // Runs decoder layers [l0, l1).  With h_in == nullptr the pass starts from the token embeddings (l0 must be 0)
 // and ends with the final norm (+ head); otherwise it starts from the given fp32 residual stream and hands the
 // residual stream after layer l1 - 1 back through h_out, with no final norm.
-static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, bool with_head, float tau,
+static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *bt, bool with_head, float tau,
                           float *scores, uint8_t *escalate, void *hidden_out, void *ws, size_t ws_bytes,
                           hipStream_t st, int l0, int l1, const float *h_in = nullptr, float *h_out = nullptr,
                           bool ws_is_static = false) {
-  if (!m || !kv) return arb_fail(ARB_EINVAL, "null model or kv");
+  if (!m || !kv.given) return arb_fail(ARB_EINVAL, "null model or kv");
   const arb_model_cfg &c = m->cfg;
   BatchInfo info;
   if (arb_status s = check_batch(bt, c.kv_block, &info, h_in == nullptr)) return s;
   if (bt->batch == 0) return ARB_OK;
   if (with_head && !scores) return arb_fail(ARB_EINVAL, "model has a router head but scores is null");
   if (!with_head && (scores || escalate)) return arb_fail(ARB_EINVAL, "scores/escalate given but no router head is applied");
-  if (!kv->k_pool || !kv->v_pool) return arb_fail(ARB_EINVAL, "null kv pool table");
-  for (int l = l0; l < l1; ++l)
-    if (!kv->k_pool[l] || !kv->v_pool[l]) return arb_fail(ARB_EINVAL, "null kv pool in layer %d", l);
+  if (!kv.k_pool || !kv.v_pool || (kv.kv8 && (!kv.k_scale || !kv.v_scale))) return arb_fail(ARB_EINVAL, "null kv pool table");
+  for (int l = l0; l < l1; ++l) {
+    if (!kv.k_pool[l] || !kv.v_pool[l]) return arb_fail(ARB_EINVAL, "null kv pool in layer %d", l);
+    if (kv.kv8 && (!kv.k_scale[l] || !kv.v_scale[l])) return arb_fail(ARB_EINVAL, "null kv scales in layer %d", l);
+    if (kv.kv8)
+      if (arb_status s = check_layer(kv.layer(l), "8-bit cache")) return s;
+  }
   const int T = bt->total_tokens, B = bt->batch, d = c.d_model;
   const int G = c.n_q_heads / c.n_kv_heads;
   AttnPlan plan = plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
@@ -276,11 +344,11 @@ static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, b
     // index with are range-checked on the device first, and this call waits for the verdict, so that a
     // bad id becomes an error instead of an out-of-bounds access.  The error word borrows the
     // workspace's partial-product area, which nothing has written yet.
-    if (kv->n_blocks <= 0) return arb_fail(ARB_EINVAL, "debug id check: arb_kv.n_blocks = %d", kv->n_blocks);
+    if (kv.n_blocks <= 0) return arb_fail(ARB_EINVAL, "debug id check: arb_kv.n_blocks = %d", kv.n_blocks);
     int32_t *err = (int32_t *)w.parts, host[4] = {0, 0, 0, 0};
     if (arb_status s0 = launch_check_ids(h_in ? nullptr : bt->token_ids, T, c.vocab, bt->block_tables, B,
                                          bt->max_blocks_per_seq, bt->prefix_lens, bt->cu_step_lens, c.kv_block,
-                                         kv->n_blocks, err, st))
+                                         kv.n_blocks, err, st))
       return s0;
     ARB_CHECK_HIP(hipMemcpyAsync(host, err, sizeof host, hipMemcpyDeviceToHost, st));
     ARB_CHECK_HIP(hipStreamSynchronize(st));
@@ -288,7 +356,7 @@ static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, b
       return arb_fail(ARB_EINVAL, "debug id check: token_ids[%d] is outside [0, %d)", host[1], c.vocab);
     if (host[0] & 2)
       return arb_fail(ARB_EINVAL, "debug id check: block_tables[%d][%d] is outside [0, %d)",
-                      host[2] / bt->max_blocks_per_seq, host[2] % bt->max_blocks_per_seq, kv->n_blocks);
+                      host[2] / bt->max_blocks_per_seq, host[2] % bt->max_blocks_per_seq, kv.n_blocks);
   }
   if (h_in) ARB_CHECK_HIP(hipMemcpyAsync(w.h, h_in, (size_t)T * d * sizeof(float), hipMemcpyDeviceToDevice, st));
 
@@ -340,7 +408,9 @@ static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, b
   };
   // Few tokens: QKV rotates and appends by itself, O completes the residual stream, and gate/up applies the norm between the two.
   const bool norms = !m->w4 && gemm_few_norms(T, d, hq, c.d_ffn);
-  const bool rotates = !m->w4 && gemm_few_rotates(T, m->qkv_rows(), d);
+  // (Its epilogue knows neither head norms nor the 8-bit cache, whose scales need a whole head.)
+  const bool head_norms = !m->g_q.empty();
+  const bool rotates = !m->w4 && !head_norms && !kv.kv8 && gemm_few_rotates(T, m->qkv_rows(), d);
   FewFusion few{};
   few.cs = w.cs;
   few.tok_slot = w.tok_slot;
@@ -376,8 +446,8 @@ static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, b
     }
     if (s) return s;
     if (rotates) {
-      few.k_pool = (bf16 *)kv->k_pool[l];
-      few.v_pool = (bf16 *)kv->v_pool[l];
+      few.k_pool = (bf16 *)kv.k_pool[l];
+      few.v_pool = (bf16 *)kv.v_pool[l];
       {
         TraceScope t(m, ARB_STAGE_QKV, st);
         s = launch_gemm_few_qkv(w.x, m->wqkv[l], w.q, T, m->qkv_rows(), d, few, st);
@@ -395,14 +465,19 @@ static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, b
       if (s) return s;
       TraceScope t(m, ARB_STAGE_ROPE_APPEND, st);
       // the queries leave the rotary kernel multiplied by log2(e)/sqrt(hd) (in fp32, before their one rounding)
-      s = launch_rope_append(w.q + (size_t)t0 * hq, w.parts, parts_of(pq), w.cs + (size_t)t0 * (c.head_dim / 2), w.tok_slot + t0,
-                             (bf16 *)kv->k_pool[l], (bf16 *)kv->v_pool[l], rows, c.n_q_heads, c.n_kv_heads, c.head_dim,
-                             attention_q_scale(c.head_dim), st);
+      if (head_norms || kv.kv8)
+        s = launch_norm_rope_append(w.q + (size_t)t0 * hq, w.parts, parts_of(pq), w.cs + (size_t)t0 * (c.head_dim / 2), w.tok_slot + t0,
+                                    kv.layer(l), head_norms ? m->g_q[l] : nullptr, head_norms ? m->g_k[l] : nullptr, c.rms_eps, rows,
+                                    c.n_q_heads, c.n_kv_heads, c.head_dim, attention_q_scale(c.head_dim), st);
+      else
+        s = launch_rope_append(w.q + (size_t)t0 * hq, w.parts, parts_of(pq), w.cs + (size_t)t0 * (c.head_dim / 2), w.tok_slot + t0,
+                               (bf16 *)kv.k_pool[l], (bf16 *)kv.v_pool[l], rows, c.n_q_heads, c.n_kv_heads, c.head_dim,
+                               attention_q_scale(c.head_dim), st);
       if (s) return s;
     }
     {
       TraceScope t(m, ARB_STAGE_ATTENTION, st);
-      s = launch_attention(w.q, hq, (const bf16 *)kv->k_pool[l], (const bf16 *)kv->v_pool[l],
+      s = launch_attention(w.q, hq, attn_cache(kv.layer(l), m->softcap),
                            bt->block_tables, bt->max_blocks_per_seq, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan,
                            w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
     }
@@ -457,7 +532,14 @@ static arb_status forward(arb_model *m, const arb_kv *kv, const arb_batch *bt, b
 extern "C" arb_status arb_score_steps(arb_model *m, const arb_kv *kv, const arb_batch *batch, float tau, float *scores,
                                       uint8_t *escalate, void *hidden_out, void *ws, size_t ws_bytes, void *stream) {
   if (!m) return arb_fail(ARB_EINVAL, "null model");
-  return forward(m, kv, batch, m->cfg.has_router_head != 0, tau, scores, escalate, hidden_out, ws, ws_bytes,
+  return forward(m, tables_of(kv), batch, m->cfg.has_router_head != 0, tau, scores, escalate, hidden_out, ws, ws_bytes,
+                 (hipStream_t)stream, 0, m->cfg.n_layers);
+}
+
+extern "C" arb_status arb_score_steps_kv8(arb_model *m, const arb_kv8 *kv, const arb_batch *batch, float tau, float *scores,
+                                          uint8_t *escalate, void *hidden_out, void *ws, size_t ws_bytes, void *stream) {
+  if (!m) return arb_fail(ARB_EINVAL, "null model");
+  return forward(m, tables_of(kv), batch, m->cfg.has_router_head != 0, tau, scores, escalate, hidden_out, ws, ws_bytes,
                  (hipStream_t)stream, 0, m->cfg.n_layers);
 }
 
@@ -495,15 +577,46 @@ extern "C" arb_status arb_score_steps_noalloc(arb_model *m, const arb_kv *kv, co
   if (arb_status s = static_scratch(&ws)) return s;
   // Nothing in the workspace is read before this call has written it (every buffer is a kernel's output
   // before it is another's input), so the previous call's contents need no clearing.
-  return forward(m, kv, batch, m->cfg.has_router_head != 0, tau, scores, escalate, hidden_out, ws,
+  return forward(m, tables_of(kv), batch, m->cfg.has_router_head != 0, tau, scores, escalate, hidden_out, ws,
                  ARB_NOALLOC_SCRATCH_BYTES, (hipStream_t)stream, 0, m->cfg.n_layers, nullptr, nullptr, true);
 }
 
 extern "C" arb_status arb_prefill(arb_model *m, const arb_kv *kv, const arb_batch *batch, void *hidden_out, void *ws,
                                   size_t ws_bytes, void *stream) {
   if (!m) return arb_fail(ARB_EINVAL, "null model");
-  return forward(m, kv, batch, false, 0.f, nullptr, nullptr, hidden_out, ws, ws_bytes, (hipStream_t)stream, 0,
+  return forward(m, tables_of(kv), batch, false, 0.f, nullptr, nullptr, hidden_out, ws, ws_bytes, (hipStream_t)stream, 0,
                  m->cfg.n_layers);
+}
+
+extern "C" arb_status arb_prefill_kv8(arb_model *m, const arb_kv8 *kv, const arb_batch *batch, void *hidden_out, void *ws,
+                                      size_t ws_bytes, void *stream) {
+  if (!m) return arb_fail(ARB_EINVAL, "null model");
+  return forward(m, tables_of(kv), batch, false, 0.f, nullptr, nullptr, hidden_out, ws, ws_bytes, (hipStream_t)stream, 0,
+                 m->cfg.n_layers);
+}
+
+static arb_status kv8_convert(const char *name, bool pack, const arb_kv_layer *src, const int32_t *src_blocks, const arb_kv_layer *dst,
+                              const int32_t *dst_blocks, int32_t n, int32_t n_kv_heads, int32_t head_dim, void *stream) {
+  if (n < 0) return arb_fail(ARB_EINVAL, "%s: n_blocks = %d", name, n);
+  if (n_kv_heads <= 0) return arb_fail(ARB_ESHAPE, "%s: n_kv_heads %d", name, n_kv_heads);
+  if (head_dim != 64 && head_dim != 128) return arb_fail(ARB_EUNSUPPORTED, "%s: head_dim %d (64 or 128 only)", name, head_dim);
+  if (n == 0) return ARB_OK;
+  if (!src || !dst) return arb_fail(ARB_EINVAL, "%s: null pointer", name);
+  if (arb_status s = check_layer(*src, name)) return s;
+  if (arb_status s = check_layer(*dst, name)) return s;
+  if ((src->k_scale != nullptr) == pack || (dst->k_scale != nullptr) != pack)
+    return arb_fail(ARB_EINVAL, "%s: the 8-bit side has scales, the bf16 side has none", name);
+  return launch_kv8_convert(pack, *src, src_blocks, *dst, dst_blocks, n, n_kv_heads, head_dim, (hipStream_t)stream);
+}
+
+extern "C" arb_status arb_kv8_pack(const arb_kv_layer *src, const int32_t *src_blocks, const arb_kv_layer *dst,
+                                   const int32_t *dst_blocks, int32_t n_blocks, int32_t n_kv_heads, int32_t head_dim, void *stream) {
+  return kv8_convert("arb_kv8_pack", true, src, src_blocks, dst, dst_blocks, n_blocks, n_kv_heads, head_dim, stream);
+}
+
+extern "C" arb_status arb_kv8_unpack(const arb_kv_layer *src, const int32_t *src_blocks, const arb_kv_layer *dst,
+                                     const int32_t *dst_blocks, int32_t n_blocks, int32_t n_kv_heads, int32_t head_dim, void *stream) {
+  return kv8_convert("arb_kv8_unpack", false, src, src_blocks, dst, dst_blocks, n_blocks, n_kv_heads, head_dim, stream);
 }
 
 extern "C" arb_status arb_route(const float *scores, int32_t n, float tau, int32_t sense, uint8_t *escalate,
@@ -637,17 +750,16 @@ extern "C" int32_t arb_gemm_large_tile_columns(int32_t M, int32_t N, int32_t K, 
   return gemm_large_cols(M, N, K, epilogue, 1);
 }
 
-extern "C" arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
-                                          const void *k_pool, const void *v_pool, const arb_batch *batch, void *out,
-                                          void *ws, size_t ws_bytes, void *stream) {
+static arb_status stage_attention(const char *name, const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
+                                  const AttnCache &cache, const arb_batch *batch, void *out, void *ws, size_t ws_bytes, void *stream) {
   if (!m) return arb_fail(ARB_EINVAL, "null model");
   const arb_model_cfg &c = m->cfg;
   BatchInfo info;
   if (arb_status s = check_batch(batch, c.kv_block, &info, false)) return s;
   if (batch->batch == 0) return ARB_OK;
-  if (!q || !k_pool || !v_pool || !out) return arb_fail(ARB_EINVAL, "arb_stage_attention: null pointer");
+  if (!q || !cache.k_pool || !cache.v_pool || !out) return arb_fail(ARB_EINVAL, "%s: null pointer", name);
   if (q_row_stride < c.n_q_heads * c.head_dim || q_row_stride % 8 != 0)
-    return arb_fail(ARB_EINVAL, "arb_stage_attention: q_row_stride %d", q_row_stride);
+    return arb_fail(ARB_EINVAL, "%s: q_row_stride %d", name, q_row_stride);
   const int G = c.n_q_heads / c.n_kv_heads, T = batch->total_tokens;
   AttnPlan plan = plan_attention(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   hipStream_t st = (hipStream_t)stream;
@@ -665,9 +777,27 @@ extern "C" arb_status arb_stage_attention(const arb_model *m, const void *q, int
                                          batch->max_blocks_per_seq, c.kv_block, nullptr, nullptr, st, &plan,
                                          attention_lists(ws, plan, T, c.n_q_heads, c.head_dim), G, c.n_kv_heads))
       return s;
-  return launch_attention((const bf16 *)q, q_row_stride, (const bf16 *)k_pool, (const bf16 *)v_pool, batch->block_tables,
+  return launch_attention((const bf16 *)q, q_row_stride, cache, batch->block_tables,
                           batch->max_blocks_per_seq, batch->batch, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out,
                           ws, ws_bytes, batch->prefix_lens, batch->cu_step_lens, st, q_scaled != 0);
+}
+
+extern "C" arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
+                                          const void *k_pool, const void *v_pool, const arb_batch *batch, void *out,
+                                          void *ws, size_t ws_bytes, void *stream) {
+  return stage_attention("arb_stage_attention", m, q, q_row_stride, q_scaled, AttnCache{k_pool, v_pool, nullptr, nullptr, 0.f},
+                         batch, out, ws, ws_bytes, stream);
+}
+
+extern "C" arb_status arb_stage_attention_kv(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
+                                             const arb_kv_layer *kv, float softcap, const arb_batch *batch, void *out, void *ws,
+                                             size_t ws_bytes, void *stream) {
+  const char *name = "arb_stage_attention_kv";
+  if (!kv) return arb_fail(ARB_EINVAL, "%s: null kv", name);
+  if (arb_status s = check_layer(*kv, name)) return s;
+  if (arb_status s = check_softcap(softcap, name)) return s;
+  if (!aligned16(q) || !aligned16(out)) return arb_fail(ARB_EINVAL, "%s: q and out are aligned to 16 bytes", name);
+  return stage_attention(name, m, q, q_row_stride, q_scaled, attn_cache(*kv, softcap), batch, out, ws, ws_bytes, stream);
 }
 
 extern "C" arb_status arb_stage_rmsnorm(const float *x, const float *g, float eps, int32_t T, int32_t d, void *out,
@@ -702,15 +832,42 @@ extern "C" arb_status arb_stage_rope_append(const arb_model *m, void *qkv, void 
                             c.n_kv_heads, c.head_dim, 1.0f, st);
 }
 
-extern "C" arb_status arb_stage_layers(arb_model *m, const arb_kv *kv, const arb_batch *batch, int32_t layer_begin,
-                                       int32_t layer_end, const float *h_in, float *h_out, void *ws, size_t ws_bytes,
-                                       void *stream) {
+extern "C" arb_status arb_stage_norm_rope_append(const arb_model *m, void *qkv, const float *g_q, const float *g_k, int32_t q_scaled,
+                                                 const arb_kv_layer *kv, const arb_batch *batch, void *q_out, void *stream) {
+  const char *name = "arb_stage_norm_rope_append";
+  if (!m) return arb_fail(ARB_EINVAL, "null model");
+  const arb_model_cfg &c = m->cfg;
+  BatchInfo info;
+  if (arb_status s = check_batch(batch, c.kv_block, &info, false)) return s;
+  if (batch->batch == 0) return ARB_OK;
+  if (!qkv || !kv) return arb_fail(ARB_EINVAL, "%s: null pointer", name);
+  if (arb_status s = check_layer(*kv, name)) return s;
+  if (!aligned16(qkv) || !aligned16(q_out) || !aligned16(g_q) || !aligned16(g_k))
+    return arb_fail(ARB_EINVAL, "%s: qkv, q_out and the gains are aligned to 16 bytes", name);
+  return launch_norm_rope_append_rows((bf16 *)qkv, (bf16 *)q_out, *kv, g_q, g_k, c.rms_eps, c.rope_base, *batch, c.n_q_heads,
+                                      c.n_kv_heads, c.head_dim, q_scaled ? attention_q_scale(c.head_dim) : 1.0f, (hipStream_t)stream);
+}
+
+static arb_status stage_layers(arb_model *m, const CacheTables &kv, const arb_batch *batch, int32_t layer_begin,
+                               int32_t layer_end, const float *h_in, float *h_out, void *ws, size_t ws_bytes, void *stream) {
   if (!m) return arb_fail(ARB_EINVAL, "null model");
   if (layer_begin < 0 || layer_end > m->cfg.n_layers || layer_begin >= layer_end)
     return arb_fail(ARB_EINVAL, "arb_stage_layers: layers [%d, %d) of %d", layer_begin, layer_end, m->cfg.n_layers);
   if (batch && batch->batch > 0 && (!h_in || !h_out)) return arb_fail(ARB_EINVAL, "arb_stage_layers: null residual stream");
   return forward(m, kv, batch, false, 0.f, nullptr, nullptr, nullptr, ws, ws_bytes, (hipStream_t)stream, layer_begin,
                  layer_end, h_in, h_out);
+}
+
+extern "C" arb_status arb_stage_layers(arb_model *m, const arb_kv *kv, const arb_batch *batch, int32_t layer_begin,
+                                       int32_t layer_end, const float *h_in, float *h_out, void *ws, size_t ws_bytes,
+                                       void *stream) {
+  return stage_layers(m, tables_of(kv), batch, layer_begin, layer_end, h_in, h_out, ws, ws_bytes, stream);
+}
+
+extern "C" arb_status arb_stage_layers_kv8(arb_model *m, const arb_kv8 *kv, const arb_batch *batch, int32_t layer_begin,
+                                           int32_t layer_end, const float *h_in, float *h_out, void *ws, size_t ws_bytes,
+                                           void *stream) {
+  return stage_layers(m, tables_of(kv), batch, layer_begin, layer_end, h_in, h_out, ws, ws_bytes, stream);
 }
 
 extern "C" arb_status arb_stage_norm_pool_head(const float *h, const float *g_final, float eps, const arb_batch *batch,

@@ -1,4 +1,4 @@
-// Ragged GQA append-attention over a block-paged bf16 KV cache.
+// Ragged GQA append-attention over a block-paged KV cache, bf16 or 8-bit, scores optionally capped.
 //
 // Work decomposition.  For sequence b and kv head hk, the G = Hq/Hkv query heads
 // that share hk and the s_b step tokens form s_b*G query rows (row = i*G + g,
@@ -21,6 +21,11 @@
 // MFMA contraction slots with keys follows the 32x32 D layout (lane half h,
 // registers 8u..8u+7 of tile t hold keys 32t+16u+4h+{0..3} and
 // 32t+16u+8+4h+{0..3}); V^T is read with the same pairing.
+//
+// An 8-bit cache (e4m3 elements, a power-of-two scale per row) goes through registers: a thread loads 16 elements of a
+// row and the row's scale, v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of two elements and the scale, exactly, and the
+// stages in LDS are those of the bf16 cache.  So a tile is converted once per workgroup, not once per wave, and the rest
+// is the same kernel: the products are, bit for bit, those over the cache's bf16 values.
 #include "common.h"
 
 #include <math.h>
@@ -65,10 +70,15 @@ __device__ __forceinline__ int v_off(int key, int chunk) { return key * HD + ((c
 // half a max3, half a dot2 (row sum over the rounded probabilities, the ones the PV product uses) and half a
 // convert per score.  Otherwise (queries as given, exact) the scale and the reference are applied to the fp32
 // scores by one FMA per score; negm[0] then holds minus the reference.
-template <int HD, bool PRESCALED>
+//
+// CAP: the logit x becomes cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), in log2 units: cap_out - 2 cap_out /
+// (exp2(cap_in s) + 1), which takes two more transcendentals per score.  The capped value is no longer linear in
+// the score, so the matrix pipe cannot start from the reference.  scale_log2 is then cap_in.
+template <int HD, bool PRESCALED, bool CAP>
 __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, const bf16x8 (&qf)[HD / 16], f32x16 (&o)[HD / 32],
                                             f32x16 &negm, float &m_run, float &l_run, int ts, int limit, float scale_log2,
-                                            int col, int half, int lane) {
+                                            float cap_out, int col, int half, int lane) {
+  static_assert(!(PRESCALED && CAP), "capped scores do not start from the reference maximum");
   constexpr int KSTEPS = HD / 16, MT = HD / 32;
   f32x16 st[2];
   if (!PRESCALED) {
@@ -97,6 +107,14 @@ __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, cons
         st[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk % 3][t], qf[kk], PRESCALED && kk == 0 ? negm : st[t], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
+  }
+  if (CAP) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        st[t][r] = fmaf(-2.f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * scale_log2) + 1.f), cap_out);
+    scale_log2 = 1.f;
   }
   // Causal mask (it also hides keys past the context): only tiles that reach some row's limit pay
   // for it.  Register r of tile t holds key ts + 32t + 8(r/4) + 4*half + r%4.
@@ -198,18 +216,38 @@ __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, cons
     }
 }
 
-template <int HD, bool SPLIT, bool PRESCALED>
+// Two neighbouring e4m3 elements times the scale of their row, as bf16: exact (four significant bits).
+template <bool HIGH>
+__device__ __forceinline__ bf16x2 e4m3_pair(uint32_t four, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, HIGH);
+}
+
+// 16 elements of a row into the two 16-byte chunks of the bf16 stage that they fill.
+__device__ __forceinline__ void store_16_e4m3(const u32x4 &v, uint32_t scale_byte, bf16 *chunk0, bf16 *chunk1) {
+  const float scale = __builtin_bit_cast(float, scale_byte << 23);
+  union { bf16x2 p[4]; bf16x8 c; } a, b;
+  a.p[0] = e4m3_pair<false>(v[0], scale); a.p[1] = e4m3_pair<true>(v[0], scale);
+  a.p[2] = e4m3_pair<false>(v[1], scale); a.p[3] = e4m3_pair<true>(v[1], scale);
+  b.p[0] = e4m3_pair<false>(v[2], scale); b.p[1] = e4m3_pair<true>(v[2], scale);
+  b.p[2] = e4m3_pair<false>(v[3], scale); b.p[3] = e4m3_pair<true>(v[3], scale);
+  *(bf16x8 *)chunk0 = a.c;
+  *(bf16x8 *)chunk1 = b.c;
+}
+
+template <int HD, bool SPLIT, bool PRESCALED, bool KV8, bool CAP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(
-    const bf16 *__restrict__ q, int q_row_stride, const bf16 *__restrict__ k_pool, const bf16 *__restrict__ v_pool,
+    const bf16 *__restrict__ q, int q_row_stride, const void *__restrict__ k_pool, const void *__restrict__ v_pool,
+    const uint8_t *__restrict__ k_scale, const uint8_t *__restrict__ v_scale, float cap_out,
     const int32_t *__restrict__ block_tables, int max_blocks, const int32_t *__restrict__ prefix_lens,
     const int32_t *__restrict__ cu, int max_qtiles, int max_splits, int kv_chunk, const AttnItem *__restrict__ items,
     int n_items, int run, int T,
     int Hq, int Hkv, float scale_log2, bf16 *__restrict__ out, bf16 *__restrict__ part_acc, float *__restrict__ part_ml) {
-  constexpr int CPK = HD / 8;              // 16-byte chunks per key
+  constexpr int CPK = KV8 ? HD / 16 : HD / 8;   // 16-byte chunks per key of the cache
   constexpr int LOADS = KT * CPK / 256;    // wave-wide 1 KB loads per wave, operand and tile
   constexpr int KPL = 64 / CPK;            // keys covered by one wave-wide load (4 or 8: inside one block)
   constexpr int KSTEPS = HD / 16;          // MFMA k-steps over the head dimension
   constexpr int MT = HD / 32;              // 32-row tiles of O^T
+  constexpr int EPC = KV8 ? 16 : 8, EB = KV8 ? 1 : 2;      // elements per chunk, bytes per element
   // Two stages of K and V; one array per stage so that LDS reads of one stage are not ordered
   // behind the direct-to-LDS loads in flight into the other.
   __shared__ __attribute__((aligned(16))) bf16 K0[KT * HD], K1[KT * HD], V0[KT * HD], V1[KT * HD];
@@ -305,13 +343,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   // depend on i or on the tile; only the (scalar) pool block does.
   const int kib = (wave_u * KPL + lkey) % ARB_KV_BLOCK;
   const int tkey = wave_u * KPL + lkey;            // tile-local key of load 0 (the others differ by multiples of 16 or 32)
-  const unsigned koff = (unsigned)(kib * HD + ((pchunk ^ k_swizzle<HD>(tkey)) << 3)) * 2u;                  // bytes
-  const unsigned voff = (unsigned)(kib * HD + ((pchunk ^ v_swizzle<HD>(tkey)) << 3)) * 2u;
+  // (8-bit rows are swizzled where they are stored into the stage)
+  const unsigned koff = (unsigned)(kib * HD + (KV8 ? pchunk * EPC : (pchunk ^ k_swizzle<HD>(tkey)) << 3)) * EB;                  // bytes
+  const unsigned voff = (unsigned)(kib * HD + (KV8 ? pchunk * EPC : (pchunk ^ v_swizzle<HD>(tkey)) << 3)) * EB;
   const int kib_tail = min(kib, last_key % ARB_KV_BLOCK);
-  const unsigned koff_tail = koff - (unsigned)((kib - kib_tail) * HD) * 2u, voff_tail = voff - (unsigned)((kib - kib_tail) * HD) * 2u;
-  const char *k_head = (const char *)(k_pool + (size_t)hk * ARB_KV_BLOCK * HD);
-  const char *v_head = (const char *)(v_pool + (size_t)hk * ARB_KV_BLOCK * HD);
-  const unsigned blk_bytes = (unsigned)Hkv * ARB_KV_BLOCK * HD * 2u;
+  const unsigned koff_tail = koff - (unsigned)((kib - kib_tail) * HD) * EB, voff_tail = voff - (unsigned)((kib - kib_tail) * HD) * EB;
+  const char *k_head = (const char *)k_pool + (size_t)hk * ARB_KV_BLOCK * HD * EB;
+  const char *v_head = (const char *)v_pool + (size_t)hk * ARB_KV_BLOCK * HD * EB;
+  const unsigned blk_bytes = (unsigned)Hkv * ARB_KV_BLOCK * HD * EB;
   auto dma = [&](bf16 *dk, bf16 *dv, int tile) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
@@ -324,25 +363,81 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
     }
   };
 
-  // Tile t is multiplied out of one stage while tile t+1 streams into the other and the block ids
-  // of tile t+2 are looked up; the barrier that ends a step also waits for the loads.
+  auto attend = [&](const bf16 *sk, const bf16 *sv, int t) {
+    if (wave_active)
+      attend_tile<HD, PRESCALED, CAP>(sk, sv, qf, o, negm, m_run, l_run, kv_begin + t * KT, limit, scale_log2, cap_out, col, half, lane);
+  };
   const int last_tile = n_tiles - 1;
-  lookup(0);
-  dma(K0, V0, 0);
-  lookup(min(1, last_tile));
-  __syncthreads();
-  for (int t = 0; t < n_tiles; t += 2) {
-    dma(K1, V1, min(t + 1, last_tile));
-    lookup(min(t + 2, last_tile));
-    __builtin_amdgcn_sched_barrier(0);
-    if (wave_active) attend_tile<HD, PRESCALED>(K0, V0, qf, o, negm, m_run, l_run, kv_begin + t * KT, limit, scale_log2, col, half, lane);
+  if constexpr (KV8) {
+    // Tile t is multiplied out of one stage; tile t+1, in registers since the last step, is converted into the other, and tile
+    // t+2 is requested into the registers that this frees.
+    u32x4 k8[LOADS], v8[LOADS];
+    uint32_t ks8[LOADS], vs8[LOADS];
+    const unsigned soff = kib, soff_tail = kib_tail;
+    auto request = [&](int tile) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const unsigned blk = first_blk + (unsigned)(tile * KT + i * 4 * KPL) / ARB_KV_BLOCK;
+        const bool tail = blk >= (unsigned)last_blk;
+        const uint64_t base = (uint64_t)(unsigned)blk_id[i] * blk_bytes;
+        const size_t srow = ((size_t)(unsigned)blk_id[i] * Hkv + hk) * ARB_KV_BLOCK;
+        k8[i] = *(const u32x4 *)(k_head + base + (tail ? koff_tail : koff));
+        v8[i] = *(const u32x4 *)(v_head + base + (tail ? voff_tail : voff));
+        ks8[i] = k_scale[srow + (tail ? soff_tail : soff)];
+        vs8[i] = v_scale[srow + (tail ? soff_tail : soff)];
+      }
+    };
+    auto convert = [&](bf16 *dk, bf16 *dv) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int key = i * 4 * KPL + tkey;
+        store_16_e4m3(k8[i], ks8[i], &dk[k_off<HD>(key, 2 * pchunk)], &dk[k_off<HD>(key, 2 * pchunk + 1)]);
+        store_16_e4m3(v8[i], vs8[i], &dv[v_off<HD>(key, 2 * pchunk)], &dv[v_off<HD>(key, 2 * pchunk + 1)]);
+      }
+    };
+    lookup(0);
+    request(0);
+    lookup(min(1, last_tile));
+    convert(K0, V0);
+    request(min(1, last_tile));
+    lookup(min(2, last_tile));
     __syncthreads();
-    if (t + 1 < n_tiles) {
-      dma(K0, V0, min(t + 2, last_tile));
+    for (int t = 0; t < n_tiles; t += 2) {
+      convert(K1, V1);
+      request(min(t + 2, last_tile));
       lookup(min(t + 3, last_tile));
       __builtin_amdgcn_sched_barrier(0);
-      if (wave_active) attend_tile<HD, PRESCALED>(K1, V1, qf, o, negm, m_run, l_run, kv_begin + (t + 1) * KT, limit, scale_log2, col, half, lane);
+      attend(K0, V0, t);
       __syncthreads();
+      if (t + 1 < n_tiles) {
+        convert(K0, V0);
+        request(min(t + 3, last_tile));
+        lookup(min(t + 4, last_tile));
+        __builtin_amdgcn_sched_barrier(0);
+        attend(K1, V1, t + 1);
+        __syncthreads();
+      }
+    }
+  } else {
+    // Tile t is multiplied out of one stage while tile t+1 streams into the other and the block ids
+    // of tile t+2 are looked up; the barrier that ends a step also waits for the loads.
+    lookup(0);
+    dma(K0, V0, 0);
+    lookup(min(1, last_tile));
+    __syncthreads();
+    for (int t = 0; t < n_tiles; t += 2) {
+      dma(K1, V1, min(t + 1, last_tile));
+      lookup(min(t + 2, last_tile));
+      __builtin_amdgcn_sched_barrier(0);
+      attend(K0, V0, t);
+      __syncthreads();
+      if (t + 1 < n_tiles) {
+        dma(K0, V0, min(t + 2, last_tile));
+        lookup(min(t + 3, last_tile));
+        __builtin_amdgcn_sched_barrier(0);
+        attend(K1, V1, t + 1);
+        __syncthreads();
+      }
     }
   }
 
@@ -571,7 +666,7 @@ AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int 
   return AttnLists{plan.n_items > 0 ? (AttnItem *)(p + align_up((size_t)total_tokens * sizeof(int32_t), 256)) : nullptr, (int32_t *)p};
 }
 
-arb_status launch_attention(const bf16 *q, int q_row_stride, const bf16 *k_pool, const bf16 *v_pool,
+arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &cache,
                             const int32_t *block_tables, int max_blocks_per_seq, int batch, int total_tokens, int n_q_heads,
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
                             const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled) {
@@ -585,20 +680,29 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const bf16 *k_pool,
   bf16 *part_acc = (bf16 *)ws;
   float *part_ml = (float *)((char *)ws + part_acc_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim));
   const AttnLists lists = split || listed ? attention_lists(ws, plan, total_tokens, n_q_heads, head_dim) : AttnLists{};
-  const float scale_log2 = attention_q_scale(head_dim);
+  // Capped scores: the kernel's scale is what the exponential of the tanh takes, 2 log2(e) / cap per unit of the logit.
+  const bool kv8 = cache.k_scale != nullptr, capped = cache.softcap > 0.f;
+  const float to_log2 = q_prescaled ? 1.0f : attention_q_scale(head_dim);
+  const float scale_log2 = capped ? 2.0f * to_log2 / cache.softcap : to_log2, cap_out = capped ? 1.44269504f * cache.softcap : 0.f;
   // A run is a group's query tiles, shortened where so few of them fit that some XCDs would get a whole run more.
   int run = plan.max_qtiles;
   if (run > kMaxRun && n_items % (8 * run) != 0 && n_items < 4 * 8 * run) run = kMaxRun;
   const dim3 grid(ceil_div(n_items, 8 * run) * 8 * run), block(256);
-#define ARB_ATTN_LAUNCH(HD, SPLIT, PRE)                                                                            \
-  hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE>), grid, block, 0, st, q, q_row_stride, k_pool, v_pool,      \
-                     block_tables, max_blocks_per_seq, prefix_lens, cu_step_lens, plan.max_qtiles, plan.max_splits,  \
-                     plan.kv_chunk, lists.items, n_items, run, total_tokens, n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml)
+#define ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP)                                                                  \
+  hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE, KV8, CAP>), grid, block, 0, st, q, q_row_stride, cache.k_pool, \
+                     cache.v_pool, cache.k_scale, cache.v_scale, cap_out, block_tables, max_blocks_per_seq, prefix_lens, \
+                     cu_step_lens, plan.max_qtiles, plan.max_splits, plan.kv_chunk, lists.items, n_items, run, total_tokens, \
+                     n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml)
+#define ARB_ATTN_FORM(HD, SPLIT, KV8)                                                                              \
+  if (capped) ARB_ATTN_LAUNCH(HD, SPLIT, false, KV8, true);                                                        \
+  else if (q_prescaled) ARB_ATTN_LAUNCH(HD, SPLIT, true, KV8, false);                                              \
+  else ARB_ATTN_LAUNCH(HD, SPLIT, false, KV8, false)
 #define ARB_ATTN_PICK(HD)                                                                                          \
-  if (split) { if (q_prescaled) ARB_ATTN_LAUNCH(HD, true, true); else ARB_ATTN_LAUNCH(HD, true, false); }          \
-  else       { if (q_prescaled) ARB_ATTN_LAUNCH(HD, false, true); else ARB_ATTN_LAUNCH(HD, false, false); }
+  if (kv8) { if (split) { ARB_ATTN_FORM(HD, true, true); } else { ARB_ATTN_FORM(HD, false, true); } }              \
+  else     { if (split) { ARB_ATTN_FORM(HD, true, false); } else { ARB_ATTN_FORM(HD, false, false); } }
   if (head_dim == 128) { ARB_ATTN_PICK(128) } else { ARB_ATTN_PICK(64) }
 #undef ARB_ATTN_PICK
+#undef ARB_ATTN_FORM
 #undef ARB_ATTN_LAUNCH
   ARB_CHECK_LAUNCH("attention");
   if (split) {

@@ -155,7 +155,13 @@ struct AttnLists {
   int32_t *tok_splits;
 };
 AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int n_q_heads, int head_dim);
-arb_status launch_attention(const bf16 *q, int q_row_stride, const bf16 *k_pool, const bf16 *v_pool,
+// The cache a launch reads: bf16 pools (no scales) or e4m3 pools with a scale byte per row, and the cap of its scores (0: none).
+struct AttnCache {
+  const void *k_pool, *v_pool;
+  const uint8_t *k_scale, *v_scale;
+  float softcap;
+};
+arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &cache,
                             const int32_t *block_tables, int max_blocks_per_seq, int batch, int total_tokens, int n_q_heads,
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
                             const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled);
@@ -213,6 +219,20 @@ arb_status launch_step_advance(const int32_t *open_rows, const int32_t *chosen, 
                                int32_t *n_next, hipStream_t st);
 arb_status launch_pack_steps(const int32_t *steps, int S, const int32_t *rows, const int32_t *cu, int n_rows, int32_t *ids,
                              hipStream_t st);
+
+// cache8.hip
+// launch_rope_append for a cache of either type (kv.k_scale null: bf16), with an RMS norm of every query and key head first where
+// its gain is given.  The projection is always read as fp32 partial products (n_parts.head > 0).
+arb_status launch_norm_rope_append(bf16 *qkv, const float *parts, RowParts n_parts, const f32x2 *cs, const int32_t *tok_slot,
+                                   const arb_kv_layer &kv, const float *g_q, const float *g_k, float eps, int T, int n_q_heads,
+                                   int n_kv_heads, int head_dim, float q_scale, hipStream_t st);
+// The same in one launch of its own: bf16 rows, slots and angles found by the launch itself; q_out null: in place.
+arb_status launch_norm_rope_append_rows(bf16 *qkv, bf16 *q_out, const arb_kv_layer &kv, const float *g_q, const float *g_k,
+                                        float eps, float rope_base, const arb_batch &bt, int n_q_heads, int n_kv_heads,
+                                        int head_dim, float q_scale, hipStream_t st);
+// Blocks of a bf16 cache into 8-bit blocks (pack), or back.
+arb_status launch_kv8_convert(bool pack, const arb_kv_layer &src, const int32_t *src_blocks, const arb_kv_layer &dst,
+                              const int32_t *dst_blocks, int n, int n_kv_heads, int head_dim, hipStream_t st);
 
 // gemm_w4.hip: 4-bit weights (offset-binary nibbles, eight k per uint32, bf16 scale per row and 128 k)
 arb_status launch_w4_quantize(const bf16 *W, int N, int K, uint32_t *packed, bf16 *scales, int bits, hipStream_t st);
