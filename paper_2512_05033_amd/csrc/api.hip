@@ -326,7 +326,10 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
   }
   const int T = bt->total_tokens, B = bt->batch, d = c.d_model;
   const int G = c.n_q_heads / c.n_kv_heads;
-  AttnPlan plan = plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
+  const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
+  const bool few_rows = attention_few_takes(attn_cache(kv.layer(l0), 0.f), max_rows);
+  AttnPlan plan = few_rows ? plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads)
+                           : plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   // the attention part is sized by this call's own split count (never above what arb_workspace_bytes assumed)
   Workspace w = carve(c, T, plan.max_splits, plan.n_items, ws);
   // Scratch that has no room for the attention work list (the static buffer's size does not follow from the batch) is used
@@ -477,9 +480,13 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
     }
     {
       TraceScope t(m, ARB_STAGE_ATTENTION, st);
-      s = launch_attention(w.q, hq, attn_cache(kv.layer(l), m->softcap),
-                           bt->block_tables, bt->max_blocks_per_seq, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan,
-                           w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
+      const AttnCache cache = attn_cache(kv.layer(l), m->softcap);
+      if (few_rows)
+        s = launch_attention_few(w.q, hq, cache, bt->block_tables, bt->max_blocks_per_seq, B, T, max_rows, c.n_q_heads, c.n_kv_heads,
+                                 c.head_dim, plan, w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
+      else
+        s = launch_attention(w.q, hq, cache, bt->block_tables, bt->max_blocks_per_seq, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan,
+                             w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
     }
     if (s) return s;
     {
@@ -761,6 +768,13 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
   if (q_row_stride < c.n_q_heads * c.head_dim || q_row_stride % 8 != 0)
     return arb_fail(ARB_EINVAL, "%s: q_row_stride %d", name, q_row_stride);
   const int G = c.n_q_heads / c.n_kv_heads, T = batch->total_tokens;
+  const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
+  if (attention_few_takes(cache, max_rows)) {
+    const AttnPlan plan = plan_attention_few(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, c.n_kv_heads);
+    return launch_attention_few((const bf16 *)q, q_row_stride, cache, batch->block_tables, batch->max_blocks_per_seq, batch->batch, T,
+                                max_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out, ws, ws_bytes, batch->prefix_lens,
+                                batch->cu_step_lens, (hipStream_t)stream, q_scaled != 0);
+  }
   AttnPlan plan = plan_attention(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   hipStream_t st = (hipStream_t)stream;
   // Writing the work list costs a single call 2 to 8 us (a forward writes it once for all layers), and it pays where it leaves out

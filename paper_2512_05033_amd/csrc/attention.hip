@@ -26,6 +26,7 @@
 // row and the row's scale, v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of two elements and the scale, exactly, and the
 // stages in LDS are those of the bf16 cache.  So a tile is converted once per workgroup, not once per wave, and the rest
 // is the same kernel: the products are, bit for bit, those over the cache's bf16 values.
+#include "attention_merge.h"
 #include "common.h"
 
 #include <math.h>
@@ -478,9 +479,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   }
 }
 
-// Merge of the split partials: out = sum_s w_s l_s o_s / sum_s w_s l_s with
-// w_s = exp2(m_s - max_s m_s) and o_s the split's normalised result.  A thread owns eight
-// consecutive elements of one (token, head) row, so a workgroup of 256 merges 2048 / HD rows.
+// Merge of the split partials.  A thread owns eight consecutive elements of one (token, head) row, so a workgroup of 256 merges
+// 2048 / HD rows.
 template <int HD>
 __global__ __launch_bounds__(256) void attention_merge_kernel(const bf16 *__restrict__ part_acc,
                                                               const float *__restrict__ part_ml,
@@ -492,49 +492,7 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(const bf16 *__rest
   if (idx >= stride) return;
   const int piece = threadIdx.x % TPR;
   const int n_splits = tok_splits[idx / Hq];               // splits that start at or before this token's position
-  float m = -INFINITY, l = 0.f;
-  float acc[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  // Splits are taken eight at a time: all their loads go out together (a loop over a run-time count waits for
-  // each before it asks for the next), then they are combined under their common maximum; groups of eight are
-  // chained by the usual online rescaling.
-  for (int s0 = 0; s0 < n_splits; s0 += 8) {
-    float2 ml[8];
-    bf16x8 v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (s0 + j < n_splits) {
-        ml[j] = *(const float2 *)(part_ml + ((s0 + j) * stride + idx) * 2);
-        v[j] = *(const bf16x8 *)(part_acc + ((s0 + j) * stride + idx) * HD + piece * 8);
-      } else {
-        ml[j] = float2{-INFINITY, 0.f};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[j][e] = (bf16)0.f;
-      }
-    }
-    float m_new = m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m_new = fmaxf(m_new, ml[j].x);
-    if (m_new == -INFINITY) continue;                      // no key of these splits is visible to the row
-    const float keep = exp2f(m - m_new);                   // m = -inf: 0
-    m = m_new;
-    l *= keep;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= keep;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float w = exp2f(ml[j].x - m_new) * ml[j].y;    // a split without visible keys: exp2(-inf) * 0 = 0
-      l += w;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += w * (float)v[j][e];
-    }
-  }
-  const float inv = 1.0f / l;
-  bf16x8 r;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (bf16)(acc[e] * inv);
-  *(bf16x8 *)(out + idx * HD + piece * 8) = r;
+  merge_splits<HD>(part_acc, part_ml, stride, idx, piece, n_splits, out);
 }
 
 }  // namespace
@@ -648,7 +606,7 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
 
 // Workspace: partial results [splits, T, Hq, hd] bf16 and their (m, l) fp32 (none with a single split), the splits of every
 // token, the work list (none with n_items == 0).
-static size_t part_acc_bytes(int max_splits, int T, int Hq, int hd) {
+size_t attention_part_bytes(int max_splits, int T, int Hq, int hd) {
   return max_splits > 1 ? align_up((size_t)max_splits * T * Hq * hd * sizeof(bf16), 256) : 0;
 }
 static size_t part_ml_bytes(int max_splits, int T, int Hq) {
@@ -656,12 +614,12 @@ static size_t part_ml_bytes(int max_splits, int T, int Hq) {
 }
 
 size_t attention_ws_bytes(int max_splits, size_t n_items, int total_tokens, int n_q_heads, int head_dim) {
-  return part_acc_bytes(max_splits, total_tokens, n_q_heads, head_dim) + part_ml_bytes(max_splits, total_tokens, n_q_heads) +
+  return attention_part_bytes(max_splits, total_tokens, n_q_heads, head_dim) + part_ml_bytes(max_splits, total_tokens, n_q_heads) +
          align_up((size_t)total_tokens * sizeof(int32_t), 256) + align_up(n_items * sizeof(AttnItem), 256);
 }
 
 AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int n_q_heads, int head_dim) {
-  char *p = (char *)ws + part_acc_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim) +
+  char *p = (char *)ws + attention_part_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim) +
             part_ml_bytes(plan.max_splits, total_tokens, n_q_heads);
   return AttnLists{plan.n_items > 0 ? (AttnItem *)(p + align_up((size_t)total_tokens * sizeof(int32_t), 256)) : nullptr, (int32_t *)p};
 }
@@ -678,7 +636,7 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
     return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
   const int n_items = listed ? plan.n_items : batch * plan.max_splits * n_kv_heads * plan.max_qtiles;
   bf16 *part_acc = (bf16 *)ws;
-  float *part_ml = (float *)((char *)ws + part_acc_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim));
+  float *part_ml = (float *)((char *)ws + attention_part_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim));
   const AttnLists lists = split || listed ? attention_lists(ws, plan, total_tokens, n_q_heads, head_dim) : AttnLists{};
   // Capped scores: the kernel's scale is what the exponential of the tanh takes, 2 log2(e) / cap per unit of the logit.
   const bool kv8 = cache.k_scale != nullptr, capped = cache.softcap > 0.f;
