@@ -6,7 +6,6 @@ shared library is missing, loading raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -221,6 +220,7 @@ class Model:
         _check(lib.arb_model_create(C.byref(self.cfg), C.byref(cw), C.byref(self.handle)))
         self.weights = w
         self.device = w.embed.device
+        self.q_width, self.kv_heads = n_q_heads * head_dim, (n_kv_heads, head_dim)
         try:
             if head_norms is not None:
                 for gains in head_norms:
@@ -277,6 +277,9 @@ class KVLayer:
             if _dev(t, torch.uint8).shape != k_pool.shape[:3]:
                 raise ValueError(f"scales are {tuple(k_pool.shape[:3])}, got {tuple(t.shape)}")
         self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
+        self.n_blocks, self.heads, self.device_index = k_pool.shape[0], (k_pool.shape[1], k_pool.shape[3]), k_pool.get_device()
+        if any(t.get_device() != self.device_index for t in (v_pool, k_scale, v_scale) if t is not None):
+            raise ValueError("a layer's pools and scales are on one device")
         self.c = _KVLayer(_ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale))
 
 
@@ -338,18 +341,21 @@ def _by_cache(kv, name: str):
     return getattr(load_library(), name + ("_kv8" if isinstance(kv, KVCache8) else ""))
 
 
-def _on(stream):
-    """Where outputs and scratch of a call are allocated: on the stream that the call runs on, so that neither memory still in
-    use there is handed out nor this memory is handed on before the call has run."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+def _fits(t: torch.Tensor, dtype, device_index: int) -> bool:
+    return t.dtype is dtype and t.get_device() == device_index and t.is_contiguous()
 
 
-def _here(*tensors):
-    """The library works on the current device; tensors elsewhere are refused."""
+def _current_device(*device_indices: int) -> int:
+    """The library works on the current device; what lives elsewhere is refused."""
     here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+    for i in device_indices:
+        if i != here:
+            raise ValueError(f"a tensor is on device {i}, the current device is cuda:{here}")
+    return here
+
+
+def _stream_on(stream, device_index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device_index) if stream is None else stream.cuda_stream
 
 
 def arb_score_steps(model: Model, kv: KVCache, batch: DeviceBatch, tau: float, *, want_hidden: bool = False,
@@ -605,29 +611,41 @@ def arb_stage_rope_append(model: Model, qkv: torch.Tensor, k_pool: torch.Tensor,
                                                 ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
-def _check_layer(model: Model, kv: KVLayer):
-    if kv.k_pool.shape[1] != model.cfg.n_kv_heads or kv.k_pool.shape[3] != model.cfg.head_dim:
-        raise ValueError(f"pools of shape {tuple(kv.k_pool.shape)} for {model.cfg.n_kv_heads} kv heads of {model.cfg.head_dim}")
+def _stage_device(model: Model, kv: KVLayer, batch: DeviceBatch) -> int:
+    """What the two stages below ask of their arguments first -> the device they run on."""
+    if kv.heads != model.kv_heads:
+        raise ValueError(f"pools of shape {tuple(kv.k_pool.shape)} for {model.kv_heads[0]} kv heads of {model.kv_heads[1]}")
+    return _current_device(kv.device_index, batch.tables.get_device())
+
+
+def _empty(stream, *shape, dtype, device):
+    """Outputs and scratch of a call are allocated on the stream that it runs on, so that neither memory still in use there is
+    handed out nor this memory is handed on before the call has run."""
+    if stream is None:
+        return torch.empty(*shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(*shape, dtype=dtype, device=device)
 
 
 def arb_stage_attention_kv(model: Model, q: torch.Tensor, kv: KVLayer, batch: DeviceBatch, softcap: float = 0.0,
                            ws: Optional[torch.Tensor] = None, stream=None, q_scaled: bool = False,
                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """arb_stage_attention over one layer of either type of cache, scores capped by softcap * tanh(x / softcap) if softcap > 0.
-    q bf16 [T, row] whose first Hq*hd columns are the (rotated) query heads -> bf16 [T, Hq*hd]."""
-    T, width = batch.total_tokens, model.cfg.n_q_heads * model.cfg.head_dim
-    _check_layer(model, kv)
-    if _dev(q, torch.bfloat16).dim() != 2 or q.shape[0] < T or q.shape[1] < width:
-        raise ValueError(f"q is bf16 [at least {T}, at least {width}], got {tuple(q.shape)}")
-    with _on(stream):
-        if out is None:
-            out = torch.empty(T, width, dtype=torch.bfloat16, device=q.device)
-        ws = _workspace(model, batch, ws)
-    if _dev(out, torch.bfloat16).numel() < T * width:
-        raise ValueError(f"out holds {out.numel()} elements, need {T * width}")
-    _here(q, kv.k_pool, out, ws, batch.tables)
-    _check(load_library().arb_stage_attention_kv(model.handle, q.data_ptr(), q.shape[1], int(q_scaled), C.byref(kv.c), softcap,
-                                                 C.byref(batch.c), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    q bf16 [at least T, row] whose first Hq*hd columns are the (rotated) query heads -> bf16 [T, Hq*hd]."""
+    dev, T, width = _stage_device(model, kv, batch), batch.total_tokens, model.q_width
+    if not _fits(q, torch.bfloat16, dev) or q.dim() != 2 or q.shape[0] < T or q.shape[1] < width:
+        raise ValueError(f"q is contiguous bf16 [at least {T}, at least {width}], got {q.dtype} {tuple(q.shape)} on {q.device}")
+    if out is None:
+        out = _empty(stream, T, width, dtype=torch.bfloat16, device=q.device)
+    elif not _fits(out, torch.bfloat16, dev) or out.numel() < T * width:
+        raise ValueError(f"out is contiguous bf16 of at least {T * width} elements, got {out.dtype} {tuple(out.shape)} on {out.device}")
+    if ws is None:
+        n = model.workspace_bytes(batch.batch, T, batch.max_ctx)
+        ws = _empty(stream, max(n, 256), dtype=torch.uint8, device=q.device)
+    elif not _fits(ws, torch.uint8, dev):
+        raise ValueError(f"ws is contiguous uint8, got {ws.dtype} on {ws.device}")
+    _check(load_library().arb_stage_attention_kv(model.handle, q.data_ptr(), q.shape[1], q_scaled, kv.c, softcap, batch.c,
+                                                 out.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(stream, dev)))
     return out
 
 
@@ -636,53 +654,51 @@ def arb_stage_norm_rope_append(model: Model, qkv: torch.Tensor, kv: KVLayer, bat
                                in_place: bool = False, stream=None) -> torch.Tensor:
     """Norms (where a gain, fp32 [hd], is given) and rotates the q and k heads of qkv (bf16 [T, (Hq+2Hkv)*hd]), stores k and v in
     the layer's pools and returns the queries: bf16 [T, Hq*hd], or qkv itself with in_place."""
-    T, c = batch.total_tokens, model.cfg
-    width = c.n_q_heads * c.head_dim
-    _check_layer(model, kv)
-    if tuple(_dev(qkv, torch.bfloat16).shape) != (T, (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim):
-        raise ValueError(f"qkv has shape {tuple(qkv.shape)}")
+    dev, T, width, hkv, hd = _stage_device(model, kv, batch), batch.total_tokens, model.q_width, *model.kv_heads
+    if not _fits(qkv, torch.bfloat16, dev) or qkv.shape != (T, width + 2 * hkv * hd):
+        raise ValueError(f"qkv is contiguous bf16 {(T, width + 2 * hkv * hd)}, got {qkv.dtype} {tuple(qkv.shape)} on {qkv.device}")
     for g in (g_q, g_k):
-        if g is not None and tuple(_dev(g, torch.float32).shape) != (c.head_dim,):
-            raise ValueError(f"a gain has shape {tuple(g.shape)}")
-    if in_place and out is not None:
-        raise ValueError("in_place or out, not both")
-    if out is None and not in_place:
-        with _on(stream):
-            out = torch.empty(T, width, dtype=torch.bfloat16, device=qkv.device)
-    elif out is not None and tuple(_dev(out, torch.bfloat16).shape) != (T, width):
-        raise ValueError(f"out has shape {tuple(out.shape)}")
-    _here(qkv, kv.k_pool, out, g_q, g_k, batch.tables)
-    _check(load_library().arb_stage_norm_rope_append(model.handle, qkv.data_ptr(), _ptr(g_q), _ptr(g_k), int(q_scaled),
-                                                     C.byref(kv.c), C.byref(batch.c), _ptr(out), _stream(stream)))
+        if g is not None and (not _fits(g, torch.float32, dev) or g.shape != (hd,)):
+            raise ValueError(f"a gain is fp32 [{hd}], got {g.dtype} {tuple(g.shape)} on {g.device}")
+    if in_place:
+        if out is not None:
+            raise ValueError("in_place or out, not both")
+    elif out is None:
+        out = _empty(stream, T, width, dtype=torch.bfloat16, device=qkv.device)
+    elif not _fits(out, torch.bfloat16, dev) or out.shape != (T, width):
+        raise ValueError(f"out is contiguous bf16 {(T, width)}, got {out.dtype} {tuple(out.shape)} on {out.device}")
+    _check(load_library().arb_stage_norm_rope_append(model.handle, qkv.data_ptr(), _ptr(g_q), _ptr(g_k), q_scaled, kv.c, batch.c,
+                                                     _ptr(out), _stream_on(stream, dev)))
     return qkv if in_place else out
 
 
-def _kv8_convert(entry: str, src: KVLayer, dst: KVLayer, src_blocks, dst_blocks, n_blocks, stream):
-    if src.k_pool.shape[1:] != dst.k_pool.shape[1:]:
+def _kv8_convert(entry, src: KVLayer, dst: KVLayer, src_blocks, dst_blocks, n_blocks, stream):
+    if src.heads != dst.heads:
         raise ValueError(f"pools of shape {tuple(src.k_pool.shape)} and {tuple(dst.k_pool.shape)}")
-    lists = [b for b in (src_blocks, dst_blocks) if b is not None]
+    dev = _current_device(src.device_index, dst.device_index)
     if n_blocks is None:
-        n_blocks = lists[0].numel() if lists else src.k_pool.shape[0]
-    for blocks, kv in ((src_blocks, src), (dst_blocks, dst)):
-        room = kv.k_pool.shape[0] if blocks is None else _dev(blocks, torch.int32).numel()
+        n_blocks = next((b.numel() for b in (src_blocks, dst_blocks) if b is not None), src.n_blocks)
+    for blocks, room in ((src_blocks, src.n_blocks), (dst_blocks, dst.n_blocks)):
+        if blocks is not None:
+            if not _fits(blocks, torch.int32, dev):
+                raise ValueError(f"block ids are contiguous int32, got {blocks.dtype} on {blocks.device}")
+            room = blocks.numel()
         if n_blocks > room:
             raise ValueError(f"{n_blocks} blocks, but a {'pool' if blocks is None else 'list'} of {room}")
-    _here(src.k_pool, dst.k_pool, *lists)
-    _check(getattr(load_library(), entry)(C.byref(src.c), _ptr(src_blocks), C.byref(dst.c), _ptr(dst_blocks), n_blocks,
-                                          src.k_pool.shape[1], src.k_pool.shape[3], _stream(stream)))
+    _check(entry(src.c, _ptr(src_blocks), dst.c, _ptr(dst_blocks), n_blocks, src.heads[0], src.heads[1], _stream_on(stream, dev)))
 
 
 def arb_kv8_pack(src: KVLayer, dst: KVLayer, src_blocks: Optional[torch.Tensor] = None, dst_blocks: Optional[torch.Tensor] = None,
                  n_blocks: Optional[int] = None, stream=None) -> None:
     """bf16 blocks src_blocks[i] of src into the 8-bit blocks dst_blocks[i] of dst (int32 device tensors; None: block i),
     i < n_blocks (default: the lists' length, or the whole source)."""
-    _kv8_convert("arb_kv8_pack", src, dst, src_blocks, dst_blocks, n_blocks, stream)
+    _kv8_convert(load_library().arb_kv8_pack, src, dst, src_blocks, dst_blocks, n_blocks, stream)
 
 
 def arb_kv8_unpack(src: KVLayer, dst: KVLayer, src_blocks: Optional[torch.Tensor] = None, dst_blocks: Optional[torch.Tensor] = None,
                    n_blocks: Optional[int] = None, stream=None) -> None:
     """8-bit blocks back into bf16 blocks, exactly; arguments as arb_kv8_pack."""
-    _kv8_convert("arb_kv8_unpack", src, dst, src_blocks, dst_blocks, n_blocks, stream)
+    _kv8_convert(load_library().arb_kv8_unpack, src, dst, src_blocks, dst_blocks, n_blocks, stream)
 
 
 def arb_stage_norm_pool_head(h: torch.Tensor, g_final: torch.Tensor, eps: float, batch: DeviceBatch,

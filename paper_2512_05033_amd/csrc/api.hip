@@ -202,7 +202,8 @@ struct Workspace {
 };
 
 // attn_splits, attn_items: the number of key splits whose partial results, and of work items, the attention part must hold.
-static Workspace carve(const arb_model_cfg &c, int T, int attn_splits, size_t attn_items, void *base) {
+// least_attn: bytes of the attention part at least.
+static Workspace carve(const arb_model_cfg &c, int T, int attn_splits, size_t attn_items, void *base, size_t least_attn = 0) {
   Workspace w;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -223,6 +224,7 @@ static Workspace carve(const arb_model_cfg &c, int T, int attn_splits, size_t at
   const size_t qkv_rows = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
   w.parts = (float *)take((8 * t * c.d_model > qkv_rows ? 8 * t * c.d_model : qkv_rows) * sizeof(float));
   w.attn_ws_bytes = attention_ws_bytes(attn_splits, attn_items, T, c.n_q_heads, c.head_dim);
+  if (w.attn_ws_bytes < least_attn) w.attn_ws_bytes = least_attn;
   w.attn_ws = take(w.attn_ws_bytes);
   w.total = off;
   return w;
@@ -234,7 +236,11 @@ extern "C" size_t arb_workspace_bytes(const arb_model *m, int32_t max_batch, int
   const int splits = attention_splits_cap(max_ctx), G = m->cfg.n_q_heads / m->cfg.n_kv_heads;
   // query tiles: ceil(s_b G / 128) summed over the batch, each against at most `splits` parts of its context
   const size_t items = ((size_t)max_total_tokens * G / ATTN_QROWS + max_batch) * m->cfg.n_kv_heads * splits;
-  return carve(m->cfg, max_total_tokens, splits, items, nullptr).total;
+  // calls of few rows per sequence and kv head (only those have tokens enough for nothing else) cut a context into up to one part more
+  const long long few_tokens = (long long)max_batch * (kFewRows / G);
+  const int few = few_tokens < max_total_tokens ? (int)few_tokens : max_total_tokens;
+  const size_t few_bytes = attention_ws_bytes(attention_few_parts_cap(max_ctx), 0, few, m->cfg.n_q_heads, m->cfg.head_dim);
+  return carve(m->cfg, max_total_tokens, splits, items, nullptr, few_bytes).total;
 }
 
 // --------------------------------------------------------------- batch validation
@@ -328,7 +334,9 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
   const int G = c.n_q_heads / c.n_kv_heads;
   const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
   const bool few_rows = attention_few_takes(attn_cache(kv.layer(l0), 0.f), max_rows);
-  AttnPlan plan = few_rows ? plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads)
+  FewPlan few_plan{};
+  if (few_rows) few_plan = plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows);
+  AttnPlan plan = few_rows ? AttnPlan{few_plan.per * ATTN_KT, few_plan.parts, 1, 0}
                            : plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   // the attention part is sized by this call's own split count (never above what arb_workspace_bytes assumed)
   Workspace w = carve(c, T, plan.max_splits, plan.n_items, ws);
@@ -483,7 +491,7 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
       const AttnCache cache = attn_cache(kv.layer(l), m->softcap);
       if (few_rows)
         s = launch_attention_few(w.q, hq, cache, bt->block_tables, bt->max_blocks_per_seq, B, T, max_rows, c.n_q_heads, c.n_kv_heads,
-                                 c.head_dim, plan, w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
+                                 c.head_dim, few_plan, w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
       else
         s = launch_attention(w.q, hq, cache, bt->block_tables, bt->max_blocks_per_seq, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan,
                              w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
@@ -770,7 +778,7 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
   const int G = c.n_q_heads / c.n_kv_heads, T = batch->total_tokens;
   const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
   if (attention_few_takes(cache, max_rows)) {
-    const AttnPlan plan = plan_attention_few(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, c.n_kv_heads);
+    const FewPlan plan = plan_attention_few(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows);
     return launch_attention_few((const bf16 *)q, q_row_stride, cache, batch->block_tables, batch->max_blocks_per_seq, batch->batch, T,
                                 max_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out, ws, ws_bytes, batch->prefix_lens,
                                 batch->cu_step_lens, (hipStream_t)stream, q_scaled != 0);

@@ -492,7 +492,10 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(const bf16 *__rest
   if (idx >= stride) return;
   const int piece = threadIdx.x % TPR;
   const int n_splits = tok_splits[idx / Hq];               // splits that start at or before this token's position
-  merge_splits<HD>(part_acc, part_ml, stride, idx, piece, n_splits, out);
+  SplitSum sum;
+  sum.clear();
+  sum.add<HD>(part_acc, part_ml, stride, idx, piece, 0, 1, n_splits);
+  sum.store(out + idx * HD + piece * 8);
 }
 
 }  // namespace

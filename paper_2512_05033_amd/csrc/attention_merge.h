@@ -5,52 +5,69 @@
 
 #include <math.h>
 
-// One (token, head) row: out = sum_s w_s l_s o_s / sum_s w_s l_s with w_s = exp2(m_s - max_s m_s) and o_s the split's
+// Of one (token, head) row: sum_s w_s l_s o_s and sum_s w_s l_s with w_s = exp2(m_s - m), m = max_s m_s and o_s the split's
 // normalised result.  A thread owns eight consecutive elements (`piece`) of the row; idx = token * Hq + head, stride = T * Hq.
-template <int HD>
-__device__ __forceinline__ void merge_splits(const bf16 *__restrict__ part_acc, const float *__restrict__ part_ml, size_t stride,
-                                             size_t idx, int piece, int n_splits, bf16 *__restrict__ out) {
-  float m = -INFINITY, l = 0.f;
-  float acc[8];
+struct SplitSum {
+  float m, l, acc[8];
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  // Splits are taken eight at a time: all their loads go out together (a loop over a run-time count waits for
-  // each before it asks for the next), then they are combined under their common maximum; groups of eight are
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  }
+  // Splits first, first + step, ... below n_splits, eight at a time: all their loads go out together (a loop over a run-time count
+  // waits for each before it asks for the next), then they are combined under their common maximum; groups of eight are
   // chained by the usual online rescaling.
-  for (int s0 = 0; s0 < n_splits; s0 += 8) {
-    float2 ml[8];
-    bf16x8 v[8];
+  template <int HD>
+  __device__ __forceinline__ void add(const bf16 *__restrict__ part_acc, const float *__restrict__ part_ml, size_t stride,
+                                      size_t idx, int piece, int first, int step, int n_splits) {
+    for (int s0 = first; s0 < n_splits; s0 += 8 * step) {
+      float2 ml[8];
+      bf16x8 v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (s0 + j < n_splits) {
-        ml[j] = *(const float2 *)(part_ml + ((s0 + j) * stride + idx) * 2);
-        v[j] = *(const bf16x8 *)(part_acc + ((s0 + j) * stride + idx) * HD + piece * 8);
-      } else {
-        ml[j] = float2{-INFINITY, 0.f};
+      for (int j = 0; j < 8; ++j) {
+        const int s = s0 + j * step;
+        if (s < n_splits) {
+          ml[j] = *(const float2 *)(part_ml + (s * stride + idx) * 2);
+          v[j] = *(const bf16x8 *)(part_acc + (s * stride + idx) * HD + piece * 8);
+        } else {
+          ml[j] = float2{-INFINITY, 0.f};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[j][e] = (bf16)0.f;
+          for (int e = 0; e < 8; ++e) v[j][e] = (bf16)0.f;
+        }
+      }
+      float m_new = m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m_new = fmaxf(m_new, ml[j].x);
+      if (m_new == -INFINITY) continue;                    // no key of these splits is visible to the row
+      const float keep = exp2f(m - m_new);                 // m = -inf: 0
+      m = m_new;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= keep;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w = exp2f(ml[j].x - m_new) * ml[j].y;  // a split without visible keys: exp2(-inf) * 0 = 0
+        l += w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += w * (float)v[j][e];
       }
     }
-    float m_new = m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m_new = fmaxf(m_new, ml[j].x);
-    if (m_new == -INFINITY) continue;                      // no key of these splits is visible to the row
-    const float keep = exp2f(m - m_new);                   // m = -inf: 0
-    m = m_new;
-    l *= keep;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= keep;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float w = exp2f(ml[j].x - m_new) * ml[j].y;    // a split without visible keys: exp2(-inf) * 0 = 0
-      l += w;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += w * (float)v[j][e];
-    }
   }
-  const float inv = 1.0f / l;
-  bf16x8 r;
+  // Another thread's sum: m, l and the eight accumulators in a row.
+  __device__ __forceinline__ void join(const float *x) {
+    const float m_new = fmaxf(m, x[0]);
+    const float keep = m == -INFINITY ? 0.f : exp2f(m - m_new), w = x[0] == -INFINITY ? 0.f : exp2f(x[0] - m_new);
+    m = m_new;
+    l = l * keep + x[1] * w;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (bf16)(acc[e] * inv);
-  *(bf16x8 *)(out + idx * HD + piece * 8) = r;
-}
+    for (int e = 0; e < 8; ++e) acc[e] = acc[e] * keep + x[2 + e] * w;
+  }
+  __device__ __forceinline__ void store(bf16 *dst) const {
+    const float inv = 1.0f / l;
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (bf16)(acc[e] * inv);
+    *(bf16x8 *)dst = r;
+  }
+};

@@ -109,3 +109,15 @@ REPLANNED = [
     (W.ROUTER_1P5B, [3119, 4555, 5707, 305, 950, 4955], [94, 25, 31, 87, 42, 28]),       # ragged
     (W.TARGET_8B, [5002, 3954, 2229], [9, 70, 35]),
     (W.TINY, [3060, 1467, 3282, 4631, 901, 1897, 1907, 4806, 3517, 2456, 4768], [97, 15, 89, 23, 64, 94, 40, 66, 36, 76, 49])]
+
+
+class FewPlan(C.Structure):
+    _fields_ = [("per", C.c_int), ("in_a_row", C.c_int), ("parts", C.c_int), ("groups", C.c_longlong), ("tiles", C.c_longlong)]
+
+
+def few_plan(lib, n_kv_heads, head_dim, prefix, steps, max_rows) -> FewPlan:
+    """What the library plans for an attention launch of few query rows over an 8-bit cache (a host function that the header does not declare)."""
+    f = lib._Z18plan_attention_fewiPKiS0_iii
+    f.restype, f.argtypes = FewPlan, [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int]
+    p, cu = np.asarray(prefix, np.int32), np.concatenate([[0], np.cumsum(steps)]).astype(np.int32)
+    return f(len(p), p.ctypes.data, cu.ctypes.data, n_kv_heads, head_dim, max_rows)

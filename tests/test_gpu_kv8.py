@@ -323,6 +323,22 @@ def test_attention_over_long_contexts(A, heads, prefix, steps, cap):
     check_attention(A, heads, kv, prefix, steps, 33, db, tables, cap, True)
 
 
+@pytest.mark.parametrize("heads,prefix,steps,in_a_row,parts", [
+    ("router", [130 * i % 7001 for i in range(70)], [1] * 70, 1, 10),       # workgroups that pass from pair to pair, more sequences than a wave
+    ("target", [4000, 20, 9000, 700, 64], [2, 4, 1, 3, 1], 0, 36),
+    ("tiny", [37 * i % 900 for i in range(300)], [1 + i % 8 for i in range(300)], 1, 4),
+    ("single", [5000, 1], [1, 2], 0, 20), ("target", [2048] * 16, [1] * 16, 0, 4), ("router", [767, 0, 63, 64, 500], [1, 2, 1, 1, 5], 0, 1)])
+@pytest.mark.parametrize("cap", [0.0, 12.0])
+def test_attention_of_few_rows_however_it_is_split(A, heads, prefix, steps, in_a_row, parts, cap):
+    from helpers import few_plan
+    hq, hkv, hd = HEADS[heads]
+    plan = few_plan(A.load_library(), hkv, hd, prefix, steps, max(steps) * hq // hkv)
+    assert (plan.in_a_row, plan.parts) == (in_a_row, parts)
+    db, tables, n = make_batch(A, prefix, steps, 35)
+    kv = filled(A, n, hkv, hd, 36)
+    check_attention(A, heads, kv, prefix, steps, 37, db, tables, cap, True)
+
+
 @pytest.mark.parametrize("heads,prefix,steps", [("router", [700, 64], [2, 1]), ("target", [1000], [40]), ("tiny", [333], [7])])
 @pytest.mark.parametrize("cap", [0.0, 15.0])
 def test_attention_with_scores_that_jump(A, heads, prefix, steps, cap):

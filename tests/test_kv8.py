@@ -179,3 +179,51 @@ def test_the_binding_takes_caches_of_one_kind():
         B.KVLayer(pool, pool, torch.zeros(2, 2, 16, dtype=torch.uint8))
     with pytest.raises(ValueError):
         B.KVCache8([])
+
+
+# ------------------------------------------------------------------ the split of attention over few rows
+
+def test_every_tile_of_a_decoding_batch_has_a_place(lib):
+    """Random batches: the planner ends, its workgroups cover the keys, no (sequence, kv head) is cut into more parts than it says, and
+    that is what arb_workspace_bytes counts on (one more than a part per 256 keys, 65 at most)."""
+    from helpers import few_plan
+    rng = np.random.default_rng(0)
+    seen = set()
+    for _ in range(1500):
+        batch = int(np.exp(rng.uniform(0, np.log(300))))
+        hi = int(np.exp(rng.uniform(0, np.log(200000))))
+        prefix = rng.integers(rng.integers(0, hi + 1) if rng.random() < 0.7 else hi, hi + 1, batch)
+        steps = rng.integers(1, 5, batch)
+        heads = int(rng.choice([1, 2, 8, 16]))
+        plan = few_plan(lib, heads, int(rng.choice([64, 128])), prefix, steps, int(rng.choice([4, 32])))
+        tiles = -(-(prefix + steps) // 64)
+        assert plan.tiles == tiles.sum() * heads and plan.per >= 1
+        if plan.in_a_row:
+            assert plan.groups == -(-plan.tiles // plan.per)
+            ends = np.cumsum(np.repeat(tiles, heads))
+            cuts = (ends - 1) // plan.per - (ends - np.repeat(tiles, heads)) // plan.per + 1
+            assert cuts.max() <= plan.parts
+        else:
+            assert -(-tiles.max() // plan.per) == plan.parts and plan.groups == batch * heads * plan.parts
+        assert plan.parts <= min(-(-int(tiles.max()) // 4), 64) + 1
+        seen.add((plan.in_a_row, plan.parts > 1))
+    assert len(seen) == 3                                        # in a row, even, uncut
+
+
+def test_workspace_covers_a_decoding_batch(lib):
+    """arb_workspace_bytes is enough for what a call on an 8-bit cache asks for (a refusal names it)."""
+    import re
+    from paper_2512_05033_amd import binding as B
+    w, _keep = _weights()
+    _, h = _create(lib, _cfg(), w)
+    t = (C.c_void_p * 2)(P, P)
+    kv = B._KV8(t, t, t, t, 1 << 20)
+    rng = np.random.default_rng(1)
+    for _ in range(300):
+        batch, hi = int(np.exp(rng.uniform(0, np.log(100)))), int(np.exp(rng.uniform(0, np.log(100000))))
+        prefix, steps = rng.integers(0, hi + 1, batch), rng.integers(1, int(rng.choice([2, 17, 80])), batch)
+        bt = _batch(B, prefix, np.concatenate([[0], np.cumsum(steps)]), 1 << 14)
+        assert lib.arb_score_steps_kv8(h, C.byref(kv), C.byref(bt), 0.0, P, None, None, P, 16, None) == B.ARB_ECAPACITY
+        need = int(re.search(rb"workspace 16 < (\d+) bytes", lib.arb_last_error()).group(1))
+        assert need <= lib.arb_workspace_bytes(h, batch, int(steps.sum()), int((prefix + steps).max()))
+    lib.arb_model_destroy(h)
