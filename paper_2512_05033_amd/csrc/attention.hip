@@ -72,9 +72,10 @@ __device__ __forceinline__ int v_off(int key, int chunk) { return key * HD + ((c
 // convert per score.  Otherwise (queries as given, exact) the scale and the reference are applied to the fp32
 // scores by one FMA per score; negm[0] then holds minus the reference.
 //
-// CAP: the logit x becomes cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), in log2 units: cap_out - 2 cap_out /
-// (exp2(cap_in s) + 1), which takes two more transcendentals per score.  The capped value is no longer linear in
-// the score, so the matrix pipe cannot start from the reference.  scale_log2 is then cap_in.
+// CAP: the logit x becomes cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), in log2 units: cap_out - 2 cap_out r with
+// r = 1 / (exp2(cap_in s) + 1), which takes two more transcendentals per score.  It is no longer linear in the score, so the
+// matrix pipe cannot start from the reference; but it is linear in r, so the maximum is a minimum of r, and cap and
+// reference are one FMA in front of the exponential.  scale_log2 is then cap_in.
 template <int HD, bool PRESCALED, bool CAP>
 __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, const bf16x8 (&qf)[HD / 16], f32x16 (&o)[HD / 32],
                                             f32x16 &negm, float &m_run, float &l_run, int ts, int limit, float scale_log2,
@@ -113,10 +114,9 @@ __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, cons
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        st[t][r] = fmaf(-2.f * cap_out, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * scale_log2) + 1.f), cap_out);
-    scale_log2 = 1.f;
+      for (int r = 0; r < 16; ++r) st[t][r] = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(st[t][r] * scale_log2) + 1.f);
   }
+  constexpr float kHidden = CAP ? INFINITY : -INFINITY;
   // Causal mask (it also hides keys past the context): only tiles that reach some row's limit pay
   // for it.  Register r of tile t holds key ts + 32t + 8(r/4) + 4*half + r%4.
   const int vis = limit - ts - 4 * half;
@@ -124,17 +124,18 @@ __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, cons
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[t][r] = (t * 32 + 8 * (r >> 2) + (r & 3)) <= vis ? st[t][r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) st[t][r] = (t * 32 + 8 * (r >> 2) + (r & 3)) <= vis ? st[t][r] : kHidden;
   }
   // largest logit this lane holds for its query (the positive scale commutes with max), relative to the
   // reference maximum.  A query's keys are split between lanes l and l ^ 32; the two are only combined
   // (a cross-lane exchange) on the rare path below.
-  float mx = -INFINITY;
+  float mx = kHidden;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[t][r]);
-  if (!PRESCALED) mx = fmaf(mx, scale_log2, negm[0]);
+    for (int r = 0; r < 16; ++r) mx = CAP ? fminf(mx, st[t][r]) : fmaxf(mx, st[t][r]);
+  if (CAP) mx = fmaf(-2.f * cap_out, mx, cap_out + negm[0]);
+  else if (!PRESCALED) mx = fmaf(mx, scale_log2, negm[0]);
   // The reference maximum m_run is advanced only when some row's maximum has outgrown it by more
   // than kLazyLog2: until then exp2(s - m_run) <= 2^kLazyLog2, far inside the range of bf16 and
   // fp32, and o / l is unchanged because both carry the same factor.  Most tiles then skip the
@@ -165,11 +166,11 @@ __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, cons
     m_run = m_new;
   }
   if (!PRESCALED) {
-    const float nm = negm[0];
+    const float factor = CAP ? -2.f * cap_out : scale_log2, shift = CAP ? cap_out + negm[0] : negm[0];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[t][r] = fmaf(st[t][r], scale_log2, nm);
+      for (int r = 0; r < 16; ++r) st[t][r] = fmaf(st[t][r], factor, shift);
   }
   bf16x8 pf[2][2];
 #pragma unroll
