@@ -333,9 +333,9 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
   const int T = bt->total_tokens, B = bt->batch, d = c.d_model;
   const int G = c.n_q_heads / c.n_kv_heads;
   const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
-  const bool few_rows = attention_few_takes(attn_cache(kv.layer(l0), 0.f), max_rows);
+  const bool few_rows = attention_few_takes(attn_cache(kv.layer(l0), m->softcap), c.head_dim, max_rows);
   FewPlan few_plan{};
-  if (few_rows) few_plan = plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows);
+  if (few_rows) few_plan = plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows, kv.kv8);
   AttnPlan plan = few_rows ? AttnPlan{few_plan.per * ATTN_KT, few_plan.parts, 1, 0}
                            : plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   // the attention part is sized by this call's own split count (never above what arb_workspace_bytes assumed)
@@ -777,8 +777,8 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
     return arb_fail(ARB_EINVAL, "%s: q_row_stride %d", name, q_row_stride);
   const int G = c.n_q_heads / c.n_kv_heads, T = batch->total_tokens;
   const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
-  if (attention_few_takes(cache, max_rows)) {
-    const FewPlan plan = plan_attention_few(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows);
+  if (attention_few_takes(cache, c.head_dim, max_rows)) {
+    const FewPlan plan = plan_attention_few(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows, cache.k_scale != nullptr);
     return launch_attention_few((const bf16 *)q, q_row_stride, cache, batch->block_tables, batch->max_blocks_per_seq, batch->batch, T,
                                 max_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out, ws, ws_bytes, batch->prefix_lens,
                                 batch->cu_step_lens, (hipStream_t)stream, q_scaled != 0);

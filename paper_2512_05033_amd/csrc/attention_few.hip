@@ -1,4 +1,5 @@
-// Append-attention of few query rows over the 8-bit paged KV cache: decoding, and steps of a few tokens.
+// Append-attention of few query rows over the 8-bit paged KV cache, and over the bf16 one where scores are capped: decoding, and
+// steps of a few tokens.
 //
 // With at most 32 rows per sequence and kv head the launch only streams the cache, and what bounds it is how many bytes the CUs
 // keep in flight.  So nothing goes through LDS and no wave waits for another: the four waves of a workgroup take turns at
@@ -19,7 +20,8 @@
 // O^T = V^T P^T: the lane's 16 probabilities are the two operands (keys 8 u + (0..7) of block g, u = 0, 1), so V^T wants the
 // same eight keys of one column per lane.  Lane (g, c) loads HD/16 neighbouring columns of every key of block g, makes bf16 pairs of
 // neighbouring columns of one key (v_cvt_scalef32_pk_bf16_fp8, which also applies the key's scale), and exchanges halves between
-// two keys (v_perm): row c of tile mt is column c HD/16 + mt.
+// two keys (v_perm): row c of tile mt is column c HD/16 + mt.  A bf16 cache needs no conversion: the lane's elements of step j are
+// 32 j + 8 g + (0..7), and its pairs are there as they are loaded.
 #include "attention_merge.h"
 #include "common.h"
 
@@ -31,7 +33,7 @@ constexpr float kLazyLog2 = 8.0f;            // growth of a row maximum (log2 un
 struct FewArgs {
   const bf16 *q;
   int q_row_stride;
-  const uint8_t *k_pool, *v_pool, *k_scale, *v_scale;
+  const uint8_t *k_pool, *v_pool, *k_scale, *v_scale;      // bf16: pools by bytes, no scales
   const int32_t *tables, *prefix_lens, *cu;
   int batch, max_blocks, max_splits, per, in_a_row, T, Hq, Hkv;
   float scale, cap_out;                      // scale: score -> logit in log2 units, or (CAP) -> the exponent of the tanh
@@ -84,12 +86,13 @@ __device__ __forceinline__ uint32_t pair(uint32_t w, float scale) {
 }
 __device__ __forceinline__ float scale_of(uint32_t bytes, int i) { return __builtin_bit_cast(float, (bytes >> (8 * i) & 0xffu) << 23); }
 
-template <int HD, int NQ, bool CAP>
-__global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_few_kernel(FewArgs a) {
+template <int HD, int NQ, bool KV8, bool CAP>
+__global__ __launch_bounds__(256, HD == 64 && NQ == 1 && KV8 ? 4 : 2) void attention_few_kernel(FewArgs a) {
   constexpr int KK = HD / 32;                // contraction steps of the scores
-  constexpr int KJ = HD / 64;                // 16-byte pieces of a key row per lane
-  constexpr int MT = HD / 16;                // row tiles of O^T, and bytes of a value row per lane
-  constexpr int VW = MT / 4;                 // ... in dwords
+  constexpr int EB = KV8 ? 1 : 2;            // bytes per element
+  constexpr int KJ = HD * EB / 64;           // 16-byte pieces of a key row per lane
+  constexpr int MT = HD / 16;                // row tiles of O^T, and elements of a value row per lane
+  constexpr int VW = MT * EB / 4;            // ... in dwords
   constexpr int PITCH = HD + 4;
   __shared__ __attribute__((aligned(16))) float s_o[4][16 * NQ][PITCH];
   __shared__ float s_m[4][16 * NQ], s_l[4][16 * NQ];
@@ -155,26 +158,28 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_fe
     k_id = table[min(blk + kb, a.max_blocks - 1)];
     v_id = table[min(blk + g, a.max_blocks - 1)];
   };
-  // Behind the context's last block the tile's first one is read instead (the table need not hold anything there).
+  // Behind the context's last block the tile's first one, which lane 0 has, is read instead (the table need not hold anything there).
+  // All lanes take part in the exchange: inside a condition it would read from the first lane that the condition leaves.
   auto unit_of = [&](const Stretch &x, int id, int i) {
+    const int first = __builtin_amdgcn_readlane(id, 0);
     const bool within = x.tile * (KT / ARB_KV_BLOCK) + i <= (x.ctx - 1) / ARB_KV_BLOCK;
-    return (size_t)(unsigned)(within ? id : __builtin_amdgcn_readfirstlane(id)) * a.Hkv + x.hk;
+    return (size_t)(unsigned)(within ? id : first) * a.Hkv + x.hk;
   };
   auto request_k = [&](const Stretch &x) {
     const size_t unit = unit_of(x, k_id, kb);
-    const uint8_t *src = a.k_pool + unit * (ARB_KV_BLOCK * HD) + (krow * HD + g * 16) * lanes;
-    ks = *(const u32x4 *)(a.k_scale + unit * ARB_KV_BLOCK);
+    const uint8_t *src = a.k_pool + unit * (ARB_KV_BLOCK * HD * EB) + (krow * HD * EB + g * 16) * lanes;
+    if (KV8) ks = *(const u32x4 *)(a.k_scale + unit * ARB_KV_BLOCK);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int j = 0; j < KJ; ++j) kd[t][j] = *(const u32x4 *)(src + t * 4 * HD + j * 64);
+      for (int j = 0; j < KJ; ++j) kd[t][j] = *(const u32x4 *)(src + t * 4 * HD * EB + j * 64);
   };
   auto request_v = [&](const Stretch &x) {
     const size_t unit = unit_of(x, v_id, g);
-    const uint8_t *src = a.v_pool + unit * (ARB_KV_BLOCK * HD) + c * MT * lanes;
-    vs = *(const u32x4 *)(a.v_scale + unit * ARB_KV_BLOCK);
+    const uint8_t *src = a.v_pool + unit * (ARB_KV_BLOCK * HD * EB) + c * (MT * EB) * lanes;
+    if (KV8) vs = *(const u32x4 *)(a.v_scale + unit * ARB_KV_BLOCK);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) vd[k] = *(const vword *)(src + k * HD);
+    for (int k = 0; k < 16; ++k) vd[k] = *(const vword *)(src + k * HD * EB);
   };
 
   bf16x8 qf[NQ][KK];
@@ -185,9 +190,9 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_fe
     for (int n = 0; n < NQ; ++n) {
       const int row = n * 16 + c, i = row < rows ? row / G : 0;
       limit[n] = x.prefix + i;
-      const bf16 *src = a.q + (size_t)(x.tok0 + i) * a.q_row_stride + (x.hk * G + (row < rows ? row - i * G : 0)) * HD + g * 16;
+      const bf16 *src = a.q + (size_t)(x.tok0 + i) * a.q_row_stride + (x.hk * G + (row < rows ? row - i * G : 0)) * HD + g * (KV8 ? 16 : 8);
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) qf[n][kk] = *(const bf16x8 *)(src + (kk >> 1) * 64 + (kk & 1) * 8);
+      for (int kk = 0; kk < KK; ++kk) qf[n][kk] = *(const bf16x8 *)(src + (KV8 ? (kk >> 1) * 64 + (kk & 1) * 8 : kk * 32));
     }
   };
 
@@ -230,13 +235,18 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_fe
       f32x4 st[4][NQ];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const float sc = __builtin_bit_cast(float, (ks[t] >> (8 * krow) & 0xffu) << 23);
+        const float sc = KV8 ? __builtin_bit_cast(float, (ks[t] >> (8 * krow) & 0xffu) << 23) : 0.f;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) st[t][n] = f32x4(0.f);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-          const uint32_t w0 = kd[t][kk >> 1][(kk & 1) * 2], w1 = kd[t][kk >> 1][(kk & 1) * 2 + 1];
-          const u32x4 f = {pair<false>(w0, sc), pair<true>(w0, sc), pair<false>(w1, sc), pair<true>(w1, sc)};
+          u32x4 f;
+          if (KV8) {
+            const uint32_t w0 = kd[t][kk >> 1][(kk & 1) * 2], w1 = kd[t][kk >> 1][(kk & 1) * 2 + 1];
+            f = u32x4{pair<false>(w0, sc), pair<true>(w0, sc), pair<false>(w1, sc), pair<true>(w1, sc)};
+          } else {
+            f = kd[t][kk % KJ];
+          }
 #pragma unroll
           for (int n = 0; n < NQ; ++n)
             st[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[n][kk], st[t][n], 0, 0, 0);
@@ -297,7 +307,7 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_fe
         for (int k = 0; k < 16; ++k)
           if (k >= valid) vd[k] = vword(0u);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
+        for (int d = 0; d < 4 && KV8; ++d) {
           const int bytes = min(max(valid - 4 * d, 0), 4);
           const uint32_t keep = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1;
           vs[d] = (vs[d] & keep) | (0x7f7f7f7fu & ~keep);
@@ -309,16 +319,20 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_fe
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int k = 8 * u + 2 * i;
-          const float s0 = scale_of(vs[k >> 2], k & 3), s1 = scale_of(vs[k >> 2], (k & 3) + 1);
+          const float s0 = KV8 ? scale_of(vs[k >> 2], k & 3) : 0.f, s1 = KV8 ? scale_of(vs[k >> 2], (k & 3) + 1) : 0.f;
 #pragma unroll
-          for (int w = 0; w < VW; ++w)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t lo = h ? pair<true>(vd[k][w], s0) : pair<false>(vd[k][w], s0);
-              const uint32_t hi = h ? pair<true>(vd[k + 1][w], s1) : pair<false>(vd[k + 1][w], s1);
-              vf[w * 4 + h * 2][i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-              vf[w * 4 + h * 2 + 1][i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+          for (int w = 0; w < MT / 2; ++w) {               // columns 2 w and 2 w + 1
+            uint32_t lo, hi;
+            if (KV8) {
+              lo = w & 1 ? pair<true>(vd[k][w / 2], s0) : pair<false>(vd[k][w / 2], s0);
+              hi = w & 1 ? pair<true>(vd[k + 1][w / 2], s1) : pair<false>(vd[k + 1][w / 2], s1);
+            } else {
+              lo = vd[k][w % VW];
+              hi = vd[k + 1][w % VW];
             }
+            vf[w * 2][i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+            vf[w * 2 + 1][i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+          }
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -348,7 +362,7 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 ? 4 : 2) void attention_fe
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int w = 0; w < VW; ++w) {
+        for (int w = 0; w < MT / 4; ++w) {
           const f32x4 four = {o[n][w * 4][e], o[n][w * 4 + 1][e], o[n][w * 4 + 2][e], o[n][w * 4 + 3][e]};
           *(f32x4 *)&s_o[wave][n * 16 + c][(4 * g + e) * MT + w * 4] = four;
         }
@@ -442,7 +456,12 @@ __global__ __launch_bounds__(256) void attention_few_merge_kernel(FewArgs a) {
 
 constexpr int kLeastTiles = 4;               // of a workgroup: one per wave
 
-bool attention_few_takes(const AttnCache &cache, int max_rows) { return cache.k_scale && max_rows <= kFewRows; }
+// The uncapped launch over bf16 pools is the other kernel's, whose results it has always had.  A bf16 tile of 128 columns takes the
+// registers of the second query tile.
+bool attention_few_takes(const AttnCache &cache, int head_dim, int max_rows) {
+  if (cache.k_scale) return max_rows <= kFewRows;
+  return cache.softcap > 0.f && max_rows <= (head_dim == 64 ? kFewRows : 16);
+}
 
 constexpr int kUncutTiles = 12;              // contexts up to here are one part each: three tiles a wave cost less than a merge
 
@@ -451,7 +470,7 @@ static int most_parts(int n, int per) { return (n + per - 2) / per + 1; }
 
 int attention_few_parts_cap(int max_ctx) { return attention_splits_cap(max_ctx) + 1; }
 
-FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t *cu_host, int n_kv_heads, int head_dim, int max_rows) {
+FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t *cu_host, int n_kv_heads, int head_dim, int max_rows, bool kv8) {
   auto tiles = [&](int b) { return ceil_div(prefix_host[b] + cu_host[b + 1] - cu_host[b], KT); };
   long long total = 0;
   int most = 0;
@@ -462,8 +481,8 @@ FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t 
   }
   total *= n_kv_heads;
   const int cap = attention_few_parts_cap(most * KT);      // of the parts: what arb_workspace_bytes counts on
-  // As many workgroups as are resident at once: by their registers two on a CU, four of 64 columns and one query tile.
-  const int places = 256 * (head_dim == 64 && max_rows <= 16 ? 4 : 2);
+  // As many workgroups as are resident at once: by their registers two on a CU, four of 64 columns in 8 bits and one query tile.
+  const int places = 256 * (head_dim == 64 && max_rows <= 16 && kv8 ? 4 : 2);
   const long long pairs = (long long)batch * n_kv_heads;
   const bool grid_fits = batch <= 65535 && n_kv_heads <= 65535;
   if (most <= kUncutTiles && grid_fits) return FewPlan{kUncutTiles, 0, 1, pairs, total};
@@ -506,11 +525,20 @@ arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache
     a.part_ml = (float *)((char *)ws + attention_part_bytes(plan.parts, total_tokens, n_q_heads, head_dim));
   }
   const dim3 grid = plan.in_a_row ? dim3((unsigned)plan.groups) : dim3(n_kv_heads, plan.parts, batch), block(256);
-#define ARB_FEW(HD, NQ)                                                                             \
-  if (capped) hipLaunchKernelGGL((attention_few_kernel<HD, NQ, true>), grid, block, 0, st, a);      \
-  else hipLaunchKernelGGL((attention_few_kernel<HD, NQ, false>), grid, block, 0, st, a)
-  if (head_dim == 128) { if (max_rows <= 16) { ARB_FEW(128, 1); } else { ARB_FEW(128, 2); } }
-  else                 { if (max_rows <= 16) { ARB_FEW(64, 1); } else { ARB_FEW(64, 2); } }
+#define ARB_FEW(HD, NQ)                                                                                                     \
+  if (!cache.k_scale) hipLaunchKernelGGL((attention_few_kernel<HD, NQ, false, true>), grid, block, 0, st, a);               \
+  else if (capped) hipLaunchKernelGGL((attention_few_kernel<HD, NQ, true, true>), grid, block, 0, st, a);                   \
+  else hipLaunchKernelGGL((attention_few_kernel<HD, NQ, true, false>), grid, block, 0, st, a)
+  if (!attention_few_takes(cache, head_dim, max_rows)) return arb_fail(ARB_EUNSUPPORTED, "attention of few rows: %d rows", max_rows);
+  if (head_dim == 64) {
+    if (max_rows <= 16) { ARB_FEW(64, 1); } else { ARB_FEW(64, 2); }
+  } else if (max_rows <= 16) {
+    ARB_FEW(128, 1);
+  } else if (capped) {
+    hipLaunchKernelGGL((attention_few_kernel<128, 2, true, true>), grid, block, 0, st, a);
+  } else {
+    hipLaunchKernelGGL((attention_few_kernel<128, 2, true, false>), grid, block, 0, st, a);
+  }
 #undef ARB_FEW
   ARB_CHECK_LAUNCH("attention_few");
   if (split) {

@@ -115,9 +115,9 @@ class FewPlan(C.Structure):
     _fields_ = [("per", C.c_int), ("in_a_row", C.c_int), ("parts", C.c_int), ("groups", C.c_longlong), ("tiles", C.c_longlong)]
 
 
-def few_plan(lib, n_kv_heads, head_dim, prefix, steps, max_rows) -> FewPlan:
-    """What the library plans for an attention launch of few query rows over an 8-bit cache (a host function that the header does not declare)."""
-    f = lib._Z18plan_attention_fewiPKiS0_iii
-    f.restype, f.argtypes = FewPlan, [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int]
+def few_plan(lib, n_kv_heads, head_dim, prefix, steps, max_rows, kv8=True) -> FewPlan:
+    """What the library plans for an attention launch of few query rows (a host function that the header does not declare)."""
+    f = lib._Z18plan_attention_fewiPKiS0_iiib
+    f.restype, f.argtypes = FewPlan, [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_bool]
     p, cu = np.asarray(prefix, np.int32), np.concatenate([[0], np.cumsum(steps)]).astype(np.int32)
-    return f(len(p), p.ctypes.data, cu.ctypes.data, n_kv_heads, head_dim, max_rows)
+    return f(len(p), p.ctypes.data, cu.ctypes.data, n_kv_heads, head_dim, max_rows, kv8)

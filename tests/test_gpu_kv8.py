@@ -374,18 +374,26 @@ def test_long_steps_are_the_attention_over_the_unpacked_cache_bit_for_bit(A, hea
 
 
 @pytest.mark.parametrize("heads,prefix,steps", [("router", [13, 40, 64], [1, 2, 1]), ("target", [5], [60]), ("tiny", [63, 1], [3, 1]), ("router", [600], [1])])
-@pytest.mark.parametrize("fill", [0x7f, 0xff])
-def test_slots_past_the_context_may_hold_anything(A, heads, prefix, steps, fill):
+@pytest.mark.parametrize("fill,kv8,cap", [(0x7f, True, 0.0), (0xff, True, 9.0), (0xff, False, 9.0)])
+def test_slots_past_the_context_may_hold_anything(A, heads, prefix, steps, fill, kv8, cap):
     hq, hkv, hd = HEADS[heads]
     db, tables, n = make_batch(A, prefix, steps, 61)
-    full, kv = filled(A, n, hkv, hd, 62), layer8(A, n, hkv, hd, fill=fill)
+    full, kv = filled(A, n, hkv, hd, 62, kv8), layer8(A, n, hkv, hd, fill=fill) if kv8 else layer16(A, n, hkv, hd)
+    if not kv8:
+        kv.k_pool.fill_(float("nan")), kv.v_pool.fill_(float("nan"))
     for b, (p, s) in enumerate(zip(prefix, steps)):
         for pos in range(p + s):
             at = int(tables[b, pos // 16]), slice(None), pos % 16
-            for name in ("k_pool", "v_pool", "k_scale", "v_scale"):
-                getattr(kv, name).view(torch.uint8)[at] = getattr(full, name).view(torch.uint8)[at]
+            for name in ("k_pool", "v_pool", "k_scale", "v_scale") if kv8 else ("k_pool", "v_pool"):
+                a, b_ = (getattr(x, name) for x in (kv, full))
+                a.view(torch.uint8 if kv8 else torch.int16)[at] = b_.view(torch.uint8 if kv8 else torch.int16)[at]
+    # the tables' unused entries are no block at all
+    far = tables.copy()
+    for b, (p, s) in enumerate(zip(prefix, steps)):
+        far[b, -(-(p + s) // 16):] = 2 ** 30
+    db = A.DeviceBatch(db.prefix_host, db.cu_host, far)
     q = queries(sum(steps), heads, 63, True)
-    run = lambda layer: A.arb_stage_attention_kv(stage_model(heads), q, layer, db, q_scaled=True)
+    run = lambda layer: A.arb_stage_attention_kv(stage_model(heads), q, layer, db, softcap=cap, q_scaled=True)
     assert bool(torch.isfinite(run(full)).all()) and torch.equal(run(kv), run(full))
 
 
