@@ -44,31 +44,29 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
-// A key row and a value row (eight elements each per lane, the row over LANES lanes) in the 8-bit format.
-template <int LANES>
-__device__ __forceinline__ void quantize_rows(const float (&k)[8], const float (&v)[8], uint32_t (&k8)[2], uint32_t (&v8)[2],
+// A key row and a value row (N elements each per lane, the row over LANES lanes) in the 8-bit format.
+template <int LANES, int N>
+__device__ __forceinline__ void quantize_rows(const float (&k)[N], const float (&v)[N], uint32_t (&k8)[N / 4], uint32_t (&v8)[N / 4],
                                               int &k_byte, int &v_byte) {
   uint32_t km = 0, vm = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < N; ++e) {
     km = max(km, abs_bits(k[e]));                          // as integers: a NaN is larger than an infinity
     vm = max(vm, abs_bits(v[e]));
   }
   km = row_max<LANES>(km);
   vm = row_max<LANES>(vm);
   if (max(km, vm) >= kTooLarge) {
-    k8[0] = k8[1] = 0x7f7f7f7fu;
-    v8[0] = v8[1] = 0;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) { k8[i] = 0x7f7f7f7fu; v8[i] = 0; }
     k_byte = v_byte = 127;
     return;
   }
   k_byte = scale_byte(km);
   v_byte = scale_byte(vm);
   const float ki = __builtin_bit_cast(float, (254 - k_byte) << 23), vi = __builtin_bit_cast(float, (254 - v_byte) << 23);
-  k8[0] = e4m3_four(k, ki);
-  k8[1] = e4m3_four(k + 4, ki);
-  v8[0] = e4m3_four(v, vi);
-  v8[1] = e4m3_four(v + 4, vi);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) { k8[i] = e4m3_four(k + 4 * i, ki); v8[i] = e4m3_four(v + 4 * i, vi); }
 }
 
 // ------------------------------------------------------- head norms + rotary embedding + append
@@ -106,55 +104,75 @@ struct AppendArgs {
   int T, Hq, Hkv, tokens;        // tokens: of a workgroup
 };
 
-// A unit is one query head, or one kv head's key and value, of one token: HD/8 lanes, each with the pairs (t..t+3, t+HD/2..).
-// The sum of squares and the largest magnitude are shuffles among them, and everything of a row happens
+// A unit is one query head, or one kv head's key and value, of one token: HD/2/PAIRS lanes, each with the pairs (t..t+PAIRS-1,
+// t+HD/2..).  The sum of squares and the largest magnitude are shuffles among them, and everything of a row happens
 // between one load and one store.  Bound: the projection's rows in, queries and cache rows out; with few tokens one chain of
 // memory round trips.  Without a table (a call of its own) a workgroup first finds its tokens' slots and angles, a wave a
 // token, while its first unit's loads are in flight.
-template <int HD, bool PARTS, bool TABLE, bool KV8>
+template <int HD, int PAIRS, bool PARTS, bool TABLE, bool KV8>
 __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
-  constexpr int LANES = HD / 8, HALF = HD / 2, UNITS = 256 / LANES;
-  __shared__ f32x2 s_cs[TABLE ? 1 : 4 * HALF];
+  constexpr int HALF = HD / 2, LANES = HALF / PAIRS, UNITS = 256 / LANES, N = 2 * PAIRS;
+  typedef bf16 vec_b __attribute__((ext_vector_type(PAIRS)));
+  typedef uint32_t vec_w __attribute__((ext_vector_type(PAIRS / 4)));
+  __shared__ __attribute__((aligned(16))) f32x2 s_cs[TABLE ? 1 : 4 * HALF];
   __shared__ int s_slot[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tok0 = blockIdx.x * a.tokens, n_tok = min(a.tokens, a.T - tok0);
   const int per_tok = a.Hq + a.Hkv, n_units = n_tok * per_tok, stride = gridDim.y * UNITS;
-  const int t = (tid % LANES) * 4;
+  const int t = (tid % LANES) * PAIRS;
   const int heads = a.Hq + 2 * a.Hkv;
-  float x[8], v[8];
-  auto load_head = [&](int j, int head, float (&to)[8]) {
+  float x[N], v[N];
+  auto load_head = [&](int j, int head, float (&to)[N]) {
     if (PARTS) {
       const float *p0 = a.parts + ((size_t)j * heads + head) * HD + t;
       const int n_parts = j < a.row_parts.row ? a.row_parts.head : a.row_parts.tail;
-      f32x4 lo = f32x4(0.f), hi = f32x4(0.f);
-      for (int p = 0; p < n_parts; p += 4) {
-        f32x4 pa[4], pb[4];
+      constexpr int Q = PAIRS / 4, AHEAD = 16 / PAIRS;     // 16-byte pieces; partial products asked for together
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (p + i < n_parts) {
-            pa[i] = *(const f32x4 *)(p0 + (p + i) * a.part_stride);
-            pb[i] = *(const f32x4 *)(p0 + (p + i) * a.part_stride + HALF);
-          }
+      for (int e = 0; e < N; ++e) to[e] = 0.f;
+      for (int p = 0; p < n_parts; p += AHEAD) {
+        f32x4 pa[AHEAD][Q], pb[AHEAD][Q];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (p + i < n_parts) {
-            lo += pa[i];
-            hi += pb[i];
-          }
+        for (int i = 0; i < AHEAD; ++i)
+          if (p + i < n_parts)
+#pragma unroll
+            for (int w = 0; w < Q; ++w) {
+              pa[i][w] = *(const f32x4 *)(p0 + (p + i) * a.part_stride + 4 * w);
+              pb[i][w] = *(const f32x4 *)(p0 + (p + i) * a.part_stride + HALF + 4 * w);
+            }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (p + i < n_parts)
+#pragma unroll
+            for (int e = 0; e < PAIRS; ++e) {
+              to[e] += pa[i][e / 4][e % 4];
+              to[PAIRS + e] += pb[i][e / 4][e % 4];
+            }
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { to[e] = lo[e]; to[4 + e] = hi[e]; }
     } else {
       const bf16 *src = a.qkv + ((size_t)j * heads + head) * HD + t;
-      const bf16x4 lo = *(const bf16x4 *)src, hi = *(const bf16x4 *)(src + HALF);
+      const vec_b lo = *(const vec_b *)src, hi = *(const vec_b *)(src + HALF);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { to[e] = (float)lo[e]; to[4 + e] = (float)hi[e]; }
+      for (int e = 0; e < PAIRS; ++e) { to[e] = (float)lo[e]; to[PAIRS + e] = (float)hi[e]; }
     }
   };
   auto load = [&](int u) {
     const int i = u / per_tok, h = u - i * per_tok;
     load_head(tok0 + i, h, x);                             // query heads, then key heads: unit h is head h
     if (h >= a.Hq) load_head(tok0 + i, h + a.Hkv, v);
+  };
+  auto store_b = [&](bf16 *dst, const float (&from)[N], float f) {
+    vec_b lo, hi;
+#pragma unroll
+    for (int e = 0; e < PAIRS; ++e) { lo[e] = (bf16)(from[e] * f); hi[e] = (bf16)(from[PAIRS + e] * f); }
+    *(vec_b *)dst = lo;
+    *(vec_b *)(dst + HALF) = hi;
+  };
+  auto store_w = [&](uint8_t *dst, const uint32_t (&from)[N / 4]) {
+    vec_w lo, hi;
+#pragma unroll
+    for (int w = 0; w < PAIRS / 4; ++w) { lo[w] = from[w]; hi[w] = from[PAIRS / 4 + w]; }
+    *(vec_w *)dst = lo;
+    *(vec_w *)(dst + HALF) = hi;
   };
   int u = blockIdx.y * UNITS + tid / LANES;
   if (u < n_units) load(u);
@@ -175,57 +193,56 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     const bool is_q = h < a.Hq;
     const float *g = is_q ? a.g_q : a.g_k;
     if (g) {
-      float sum = 0.f;
+      float sum[PAIRS / 4];                                // of every four pairs by itself, joined last: the same order for both widths
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
-      const float r = 1.0f / sqrtf(row_sum<LANES>(sum) * (1.0f / HD) + a.eps);
-      const f32x4 g0 = *(const f32x4 *)(g + t), g1 = *(const f32x4 *)(g + t + HALF);
+      for (int w = 0; w < PAIRS / 4; ++w) {
+        sum[w] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] *= r * g0[e];
-        x[4 + e] *= r * g1[e];
+        for (int e = 0; e < 4; ++e) sum[w] += x[4 * w + e] * x[4 * w + e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[w] += x[PAIRS + 4 * w + e] * x[PAIRS + 4 * w + e];
+        sum[w] = row_sum<LANES>(sum[w]);
+      }
+      const float r = 1.0f / sqrtf((PAIRS == 8 ? sum[0] + sum[PAIRS / 4 - 1] : sum[0]) * (1.0f / HD) + a.eps);
+#pragma unroll
+      for (int w = 0; w < PAIRS / 4; ++w) {
+        const f32x4 g0 = *(const f32x4 *)(g + t + 4 * w), g1 = *(const f32x4 *)(g + t + HALF + 4 * w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[4 * w + e] *= r * g0[e];
+          x[PAIRS + 4 * w + e] *= r * g1[e];
+        }
       }
     }
     const f32x2 *cs = TABLE ? a.cs + (size_t)j * HALF + t : s_cs + i * HALF + t;
-    const f32x4 two[2] = {*(const f32x4 *)cs, *(const f32x4 *)(cs + 2)};      // (cos, sin) of two pairs each
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float c = two[e / 2][e % 2 * 2], s = two[e / 2][e % 2 * 2 + 1], p = x[e], q = x[4 + e];
-      x[e] = p * c - q * s;
-      x[4 + e] = q * c + p * s;
+    for (int w = 0; w < PAIRS / 2; ++w) {
+      const f32x4 two = *(const f32x4 *)(cs + 2 * w);      // (cos, sin) of two pairs
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float c = two[2 * e], s = two[2 * e + 1], p = x[2 * w + e], q = x[PAIRS + 2 * w + e];
+        x[2 * w + e] = p * c - q * s;
+        x[PAIRS + 2 * w + e] = q * c + p * s;
+      }
     }
     if (is_q) {
-      bf16 *dst = PARTS ? a.qkv + ((size_t)j * a.Hq + h) * HD + t : a.q_out + (size_t)j * a.q_row + h * HD + t;
-      bf16x4 lo, hi;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { lo[e] = (bf16)(x[e] * a.q_scale); hi[e] = (bf16)(x[4 + e] * a.q_scale); }
-      *(bf16x4 *)dst = lo;
-      *(bf16x4 *)(dst + HALF) = hi;
+      store_b(PARTS ? a.qkv + ((size_t)j * a.Hq + h) * HD + t : a.q_out + (size_t)j * a.q_row + h * HD + t, x, a.q_scale);
     } else {
       const int slot = TABLE ? a.tok_slot[j] : s_slot[i];
       const size_t row = ((size_t)(slot / ARB_KV_BLOCK) * a.Hkv + (h - a.Hq)) * ARB_KV_BLOCK + slot % ARB_KV_BLOCK;
       if (KV8) {
-        uint32_t k8[2], v8[2];
+        uint32_t k8[N / 4], v8[N / 4];
         int kb, vb;
         quantize_rows<LANES>(x, v, k8, v8, kb, vb);
-        uint8_t *kd = (uint8_t *)a.k_pool + row * HD + t, *vd = (uint8_t *)a.v_pool + row * HD + t;
-        *(uint32_t *)kd = k8[0];
-        *(uint32_t *)(kd + HALF) = k8[1];
-        *(uint32_t *)vd = v8[0];
-        *(uint32_t *)(vd + HALF) = v8[1];
+        store_w((uint8_t *)a.k_pool + row * HD + t, k8);
+        store_w((uint8_t *)a.v_pool + row * HD + t, v8);
         if (t == 0) {
           a.k_scale[row] = (uint8_t)kb;
           a.v_scale[row] = (uint8_t)vb;
         }
       } else {
-        bf16 *kd = (bf16 *)a.k_pool + row * HD + t, *vd = (bf16 *)a.v_pool + row * HD + t;
-        bf16x4 k0, k1, v0, v1;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { k0[e] = (bf16)x[e]; k1[e] = (bf16)x[4 + e]; v0[e] = (bf16)v[e]; v1[e] = (bf16)v[4 + e]; }
-        *(bf16x4 *)kd = k0;
-        *(bf16x4 *)(kd + HALF) = k1;
-        *(bf16x4 *)vd = v0;
-        *(bf16x4 *)(vd + HALF) = v1;
+        store_b((bf16 *)a.k_pool + row * HD + t, x, 1.0f);
+        store_b((bf16 *)a.v_pool + row * HD + t, v, 1.0f);
       }
     }
     u += stride;
@@ -236,7 +253,9 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
 // ------------------------------------------------------------------------ conversion of blocks
 
 // Eight elements of a key row and of the value row of the same position per thread; a block of one kv head is 16 rows.
-// Bound: memory, 4 HD bytes in and 2 HD + 2 out per position and kv head, or the other way round.
+// Bound: memory, 4 HD bytes in and 2 HD + 2 out per position and kv head, or the other way round.  8192 blocks of 8 heads of 128
+// packed in 134 us (6.0 TB/s), 9000 unpacked in 177 (5.0; two thirds of it is written, a large copy moves 4.8); with stores that
+// are kept in the caches 138 and 180.
 template <int HD>
 __global__ __launch_bounds__(256) void pack_kernel(const bf16 *__restrict__ k, const bf16 *__restrict__ v,
                                                    const int32_t *__restrict__ src_blocks, uint8_t *__restrict__ k8,
@@ -255,8 +274,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const bf16 *__restrict__ k, c
   uint32_t kw[2], vw[2];
   int kb, vb;
   quantize_rows<LANES>(kf, vf, kw, vw, kb, vb);
-  *(u32x2 *)(k8 + to * HD + t) = u32x2{kw[0], kw[1]};
-  *(u32x2 *)(v8 + to * HD + t) = u32x2{vw[0], vw[1]};
+  __builtin_nontemporal_store(u32x2{kw[0], kw[1]}, (u32x2 *)(k8 + to * HD + t));
+  __builtin_nontemporal_store(u32x2{vw[0], vw[1]}, (u32x2 *)(v8 + to * HD + t));
   if (t == 0) {
     k_scale[to] = (uint8_t)kb;
     v_scale[to] = (uint8_t)vb;
@@ -286,11 +305,28 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint8_t *__restrict__
   const size_t from = ((size_t)(src_blocks ? src_blocks[n] : n) * per + in), to = ((size_t)(dst_blocks ? dst_blocks[n] : n) * per + in);
   const u32x2 kw = *(const u32x2 *)(k8 + from * HD + t), vw = *(const u32x2 *)(v8 + from * HD + t);
   const uint32_t kb = k_scale[from], vb = v_scale[from];
-  *(bf16x8 *)(k + to * HD + t) = eight_values(kw, kb);
-  *(bf16x8 *)(v + to * HD + t) = eight_values(vw, vb);
+  __builtin_nontemporal_store(eight_values(kw, kb), (bf16x8 *)(k + to * HD + t));
+  __builtin_nontemporal_store(eight_values(vw, vb), (bf16x8 *)(v + to * HD + t));
 }
 
 }  // namespace
+
+// Few tokens: a workgroup per 256 lanes of units and four pairs a lane, so that a token is one round of loads.  Many: eight pairs a
+// lane (16-byte accesses of bf16 rows) and, in a call of its own, two tokens per workgroup, whose angles two waves find at once.
+// (32/8 heads into the 8-bit cache, few / many: 600 tokens 6.2 / 7.3 us, 900 9.1 / 8.4, 3001 17.7 / 14.2 (4.8 TB/s, the rate of
+// a large copy), 12000 61.8 / 56.2.  Of the 14.2 the angles are 0.5; with one token per workgroup 17.1, with four 14.6.)
+constexpr int kAppendManyTokens = 768;
+
+template <bool PARTS, bool TABLE>
+static void launch_append(const AppendArgs &a, int head_dim, int pairs, dim3 grid, hipStream_t st) {
+  grid.y = a.tokens > 1 ? 1 : ceil_div((a.Hq + a.Hkv) * (head_dim / 2 / pairs), 256);
+#define ARB_APPEND(HD, PAIRS)                                                                                                  \
+  if (a.k_scale) hipLaunchKernelGGL((norm_rope_append_kernel<HD, PAIRS, PARTS, TABLE, true>), grid, dim3(256), 0, st, a);      \
+  else hipLaunchKernelGGL((norm_rope_append_kernel<HD, PAIRS, PARTS, TABLE, false>), grid, dim3(256), 0, st, a)
+  if (head_dim == 128) { if (pairs == 8) { ARB_APPEND(128, 8); } else { ARB_APPEND(128, 4); } }
+  else                 { if (pairs == 8) { ARB_APPEND(64, 8); } else { ARB_APPEND(64, 4); } }
+#undef ARB_APPEND
+}
 
 arb_status launch_norm_rope_append(bf16 *qkv, const float *parts, RowParts n_parts, const f32x2 *cs, const int32_t *tok_slot,
                                    const arb_kv_layer &kv, const float *g_q, const float *g_k, float eps, int T, int n_q_heads,
@@ -305,14 +341,7 @@ arb_status launch_norm_rope_append(bf16 *qkv, const float *parts, RowParts n_par
   a.cs = cs, a.tok_slot = tok_slot;
   a.k_pool = kv.k_pool, a.v_pool = kv.v_pool, a.k_scale = kv.k_scale, a.v_scale = kv.v_scale;
   a.T = T, a.Hq = n_q_heads, a.Hkv = n_kv_heads, a.tokens = 1;
-  const dim3 grid(T, ceil_div(n_q_heads + n_kv_heads, 2048 / head_dim));
-  if (head_dim == 128) {
-    if (kv.k_scale) hipLaunchKernelGGL((norm_rope_append_kernel<128, true, true, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_rope_append_kernel<128, true, true, false>), grid, dim3(256), 0, st, a);
-  } else {
-    if (kv.k_scale) hipLaunchKernelGGL((norm_rope_append_kernel<64, true, true, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_rope_append_kernel<64, true, true, false>), grid, dim3(256), 0, st, a);
-  }
+  launch_append<true, true>(a, head_dim, T >= kAppendManyTokens ? 8 : 4, dim3(T), st);
   ARB_CHECK_LAUNCH("norm_rope_append");
   return ARB_OK;
 }
@@ -332,18 +361,9 @@ arb_status launch_norm_rope_append_rows(bf16 *qkv, bf16 *q_out, const arb_kv_lay
   a.log2_base = log2((double)rope_base);
   a.k_pool = kv.k_pool, a.v_pool = kv.v_pool, a.k_scale = kv.k_scale, a.v_scale = kv.v_scale;
   a.T = T, a.Hq = n_q_heads, a.Hkv = n_kv_heads;
-  // Few tokens: a workgroup per 256 lanes of units, so that a token is one round of loads.  Many: four tokens per workgroup,
-  // whose angles are found by its four waves at once.
-  const int units = n_q_heads + n_kv_heads, per_wg = 2048 / head_dim;
-  a.tokens = T >= 1024 ? 4 : 1;
-  const dim3 grid(ceil_div(T, a.tokens), T >= 1024 ? 1 : ceil_div(units, per_wg));
-  if (head_dim == 128) {
-    if (kv.k_scale) hipLaunchKernelGGL((norm_rope_append_kernel<128, false, false, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_rope_append_kernel<128, false, false, false>), grid, dim3(256), 0, st, a);
-  } else {
-    if (kv.k_scale) hipLaunchKernelGGL((norm_rope_append_kernel<64, false, false, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_rope_append_kernel<64, false, false, false>), grid, dim3(256), 0, st, a);
-  }
+  const bool many = T >= kAppendManyTokens;
+  a.tokens = many ? 2 : 1;
+  launch_append<false, false>(a, head_dim, many ? 8 : 4, dim3(ceil_div(T, a.tokens)), st);
   ARB_CHECK_LAUNCH("norm_rope_append");
   return ARB_OK;
 }
