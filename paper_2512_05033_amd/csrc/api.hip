@@ -794,14 +794,14 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
     plan.n_items = 0;
   const size_t need = plan.max_splits > 1 || plan.n_items > 0 ? attention_ws_bytes(plan.max_splits, plan.n_items, T, c.n_q_heads, c.head_dim) : 0;
   if (need > 0 && (!ws || ws_bytes < need)) return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
-  if (need > 0)                                            // with one split a call needs no scratch
+  if (plan.n_items > 0)                                    // without a list the attention launch counts the tokens' splits by itself
     if (arb_status s = launch_token_meta(batch->prefix_lens, batch->cu_step_lens, batch->block_tables, batch->batch, T,
                                          batch->max_blocks_per_seq, c.kv_block, nullptr, nullptr, st, &plan,
                                          attention_lists(ws, plan, T, c.n_q_heads, c.head_dim), G, c.n_kv_heads))
       return s;
   return launch_attention((const bf16 *)q, q_row_stride, cache, batch->block_tables,
                           batch->max_blocks_per_seq, batch->batch, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out,
-                          ws, ws_bytes, batch->prefix_lens, batch->cu_step_lens, st, q_scaled != 0);
+                          ws, ws_bytes, batch->prefix_lens, batch->cu_step_lens, st, q_scaled != 0, plan.n_items == 0);
 }
 
 extern "C" arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,

@@ -243,7 +243,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
     const int32_t *__restrict__ block_tables, int max_blocks, const int32_t *__restrict__ prefix_lens,
     const int32_t *__restrict__ cu, int max_qtiles, int max_splits, int kv_chunk, const AttnItem *__restrict__ items,
     int n_items, int run, int T,
-    int Hq, int Hkv, float scale_log2, bf16 *__restrict__ out, bf16 *__restrict__ part_acc, float *__restrict__ part_ml) {
+    int Hq, int Hkv, float scale_log2, bf16 *__restrict__ out, bf16 *__restrict__ part_acc, float *__restrict__ part_ml,
+    int32_t *__restrict__ tok_splits) {
   constexpr int CPK = KV8 ? HD / 16 : HD / 8;   // 16-byte chunks per key of the cache
   constexpr int LOADS = KT * CPK / 256;    // wave-wide 1 KB loads per wave, operand and tile
   constexpr int KPL = 64 / CPK;            // keys covered by one wave-wide load (4 or 8: inside one block)
@@ -443,40 +444,40 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
     }
   }
 
+  // The wave's result, row-major through the LDS (the stages are free: every tile ends with a barrier), so that a store writes whole
+  // rows; straight from the accumulators it is 16-byte pieces of 32 rows.  Chunks are swizzled by the row.
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-  if (!row_ok) return;
   const size_t orow = (size_t)(tok0 + tok_i) * Hq + head;   // (token, head) index
-  if (!SPLIT) {
-    const float inv = 1.0f / l_tot;
-    bf16 *dst = out + orow * HD;
+  if (!wave_active) return;
+  // With SPLIT this is the split's own normalised result in bf16 (it lies in the hull of the values, like the output)
+  // plus its (m, l) in fp32: half the partial traffic of fp32 accumulators.
+  const float inv = !SPLIT || l_tot > 0.f ? 1.0f / l_tot : 0.f;
+  constexpr int CPR = HD / 8, RPS = 64 / CPR;               // 16-byte chunks per row, rows per store
+  bf16 *buf = wave_u == 0 ? K0 : wave_u == 1 ? K1 : wave_u == 2 ? V0 : V1;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+  for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        bf16x4 v;
+    for (int r4 = 0; r4 < 4; ++r4) {
+      bf16x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[mt][r4 * 4 + e] * inv);
-        *(bf16x4 *)(dst + mt * 32 + 8 * r4 + 4 * half) = v;
-      }
-  } else {
-    // the split's own normalised result in bf16 (it lies in the hull of the values, like the output)
-    // plus its (m, l) in fp32: half the partial traffic of fp32 accumulators
-    const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
-    bf16 *dst = part_acc + ((size_t)split * T * Hq + orow) * HD;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        bf16x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[mt][r4 * 4 + e] * inv);
-        *(bf16x4 *)(dst + mt * 32 + 8 * r4 + 4 * half) = v;
-      }
-    if (half == 0) {
-      float *ml = part_ml + ((size_t)split * T * Hq + orow) * 2;
-      ml[0] = m_run;
-      ml[1] = l_tot;
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[mt][r4 * 4 + e] * inv);
+      *(bf16x4 *)&buf[col * HD + (((mt * 4 + r4) ^ (col % CPR)) << 3) + half * 4] = v;
     }
+  bf16 *dst = SPLIT ? part_acc + (size_t)split * T * Hq * HD : out;
+  const int rows_here = min(32, rows - row0 - wave * 32), orow32 = (int)orow;
+#pragma unroll
+  for (int i = 0; i < 32 / RPS; ++i) {
+    const int r = i * RPS + lane / CPR, chunk = lane % CPR;
+    const size_t at = (size_t)(unsigned)__shfl(orow32, r, 64);
+    const bf16x8 v = *(const bf16x8 *)&buf[r * HD + ((chunk ^ (r % CPR)) << 3)];
+    if (r < rows_here) *(bf16x8 *)(dst + at * HD + chunk * 8) = v;
+  }
+  if (SPLIT && half == 0 && row_ok) {
+    float *ml = part_ml + ((size_t)split * T * Hq + orow) * 2;
+    ml[0] = m_run;
+    ml[1] = l_tot;
+    // the number of splits that the merge reads for a token, where no earlier launch has written it
+    if (tok_splits && split == 0 && hk == 0) tok_splits[tok0 + tok_i] = min(limit / attn_seq_chunk(ctx, kv_chunk) + 1, max_splits);
   }
 }
 
@@ -485,14 +486,15 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
 template <int HD>
 __global__ __launch_bounds__(256) void attention_merge_kernel(const bf16 *__restrict__ part_acc,
                                                               const float *__restrict__ part_ml,
-                                                              const int32_t *__restrict__ tok_splits, int T, int Hq,
-                                                              bf16 *__restrict__ out) {
+                                                              const int32_t *__restrict__ tok_splits, int max_splits, int T,
+                                                              int Hq, bf16 *__restrict__ out) {
   constexpr int TPR = HD / 8;                              // threads per row
   const size_t stride = (size_t)T * Hq;
   const size_t idx = (size_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;      // token * Hq + head
   if (idx >= stride) return;
   const int piece = threadIdx.x % TPR;
-  const int n_splits = tok_splits[idx / Hq];               // splits that start at or before this token's position
+  // splits that start at or before this token's position (never more than there is memory for, whatever the word holds)
+  const int n_splits = min(tok_splits[idx / Hq], max_splits);
   SplitSum sum;
   sum.clear();
   sum.add<HD>(part_acc, part_ml, stride, idx, piece, 0, 1, n_splits);
@@ -631,7 +633,7 @@ AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int 
 arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &cache,
                             const int32_t *block_tables, int max_blocks_per_seq, int batch, int total_tokens, int n_q_heads,
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
-                            const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled) {
+                            const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled, bool count_splits) {
   if (batch == 0 || total_tokens == 0) return ARB_OK;
   if (head_dim != 64 && head_dim != 128) return arb_fail(ARB_EUNSUPPORTED, "attention: head_dim %d", head_dim);
   const size_t need = attention_ws_bytes(plan.max_splits, plan.n_items, total_tokens, n_q_heads, head_dim);
@@ -654,7 +656,7 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE, KV8, CAP>), grid, block, 0, st, q, q_row_stride, cache.k_pool, \
                      cache.v_pool, cache.k_scale, cache.v_scale, cap_out, block_tables, max_blocks_per_seq, prefix_lens, \
                      cu_step_lens, plan.max_qtiles, plan.max_splits, plan.kv_chunk, lists.items, n_items, run, total_tokens, \
-                     n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml)
+                     n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml, count_splits ? lists.tok_splits : nullptr)
 #define ARB_ATTN_FORM(HD, SPLIT, KV8)                                                                              \
   if (capped) ARB_ATTN_LAUNCH(HD, SPLIT, false, KV8, true);                                                        \
   else if (q_prescaled) ARB_ATTN_LAUNCH(HD, SPLIT, true, KV8, false);                                              \
@@ -670,10 +672,10 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   if (split) {
     const dim3 mgrid(ceil_div(total_tokens * n_q_heads, 2048 / head_dim)), mblock(256);
     if (head_dim == 128)
-      hipLaunchKernelGGL((attention_merge_kernel<128>), mgrid, mblock, 0, st, part_acc, part_ml, lists.tok_splits,
+      hipLaunchKernelGGL((attention_merge_kernel<128>), mgrid, mblock, 0, st, part_acc, part_ml, lists.tok_splits, plan.max_splits,
                          total_tokens, n_q_heads, out);
     else
-      hipLaunchKernelGGL((attention_merge_kernel<64>), mgrid, mblock, 0, st, part_acc, part_ml, lists.tok_splits,
+      hipLaunchKernelGGL((attention_merge_kernel<64>), mgrid, mblock, 0, st, part_acc, part_ml, lists.tok_splits, plan.max_splits,
                          total_tokens, n_q_heads, out);
     ARB_CHECK_LAUNCH("attention_merge");
   }
