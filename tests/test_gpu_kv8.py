@@ -453,6 +453,23 @@ def test_blocks_beyond_32_bit_offsets(A):
 
 # ----------------------------------------------------------------------------------- how it is called
 
+def test_more_sequences_than_a_grid_has_planes(A):
+    heads, batch = "tiny", 70_000
+    hq, hkv, hd = HEADS[heads]
+    prefix = np.arange(batch) % 3
+    prefix[-1] = 700
+    width = 44
+    tables = (np.arange(batch, dtype=np.int32) % 50)[:, None] + np.zeros((1, width), np.int32)
+    db = A.DeviceBatch(prefix.astype(np.int32), np.arange(batch + 1, dtype=np.int32), tables)
+    kv = filled(A, 50, hkv, hd, 94)
+    q = queries(batch, heads, 95, True)
+    got = A.arb_stage_attention_kv(stage_model(heads), q, kv, db, q_scaled=True)
+    for rows_ in (slice(0, 40), slice(batch - 40, batch)):       # two ends of it, as batches of their own
+        ref, mag = attention_ref(heads, q[rows_], kv, tables[rows_], prefix[rows_].tolist(), [1] * 40, 0.0, True)
+        assert bool(((got[rows_].double().view(ref.shape) - ref).abs() <= 4.3 * U * mag + 1e-30).all())
+    assert bool(torch.isfinite(got).all())
+
+
 def test_rows_behind_the_last_sequence_stay(A):
     heads, prefix, steps = "router", [70, 9], [2, 1]
     hq, hkv, hd = HEADS[heads]
@@ -514,25 +531,28 @@ def test_two_calls_at_once_on_two_streams(A):
 
 # ------------------------------------------------------------------------------ the whole forward
 
-def _forward_session(A, w, seed, softcap, norms, kv8=True):
+def _forward_session(A, w, seed, softcap, norms, kv8=True, four_bit=False):
     m, h = w.model, H()
     batch = W.make_batch(w)
     weights = W.make_weights(m, w.seed, "cuda", gain_jitter=0.1, b_head=0.0)
+    weights_of_model = A.QuantizedWeights(weights) if four_bit else weights
     g = torch.Generator().manual_seed(seed)
     gains = tuple([(1 + 0.3 * torch.randn(m.head_dim, generator=g)).cuda() for _ in range(m.n_layers)] for _ in range(2)) if norms else None
     model = A.Model(n_layers=m.n_layers, d_model=m.d_model, n_q_heads=m.n_q_heads, n_kv_heads=m.n_kv_heads, head_dim=m.head_dim,
-                    d_ffn=m.d_ffn, vocab=m.vocab, weights=weights, rms_eps=m.rms_eps, rope_base=m.rope_base,
+                    d_ffn=m.d_ffn, vocab=m.vocab, weights=weights_of_model, rms_eps=m.rms_eps, rope_base=m.rope_base,
                     has_router_head=m.has_router_head, head_norms=gains, softcap=softcap)
     kv = A.KVCache8.empty(m.n_layers, batch.n_blocks, m.n_kv_heads, m.head_dim) if kv8 else \
         A.KVCache(*([torch.zeros(batch.n_blocks, m.n_kv_heads, 16, m.head_dim, dtype=torch.bfloat16, device="cuda") for _ in range(m.n_layers)] for _ in range(2)))
     return batch, weights, gains, model, kv, h.device_batch(batch)
 
 
-def _oracle_forward(w, weights, gains, softcap, layers, ids, prefix, cu, tables):
+def _oracle_forward(w, weights, gains, softcap, layers, ids, prefix, cu, tables, four_bit=False):
     """The oracle's forward over the keys and values that the cache really holds (an element that the GPU's bf16 activations put on
     the other side of an e4m3 border is no error of the attention).  -> (final-normed hidden states, [(k, v)] it would have stored)."""
     from helpers import oracle_model, oracle_params
     m, p = oracle_model(w.model), oracle_params(weights)
+    for name in ("wqkv", "wo", "wgu", "wd") if four_bit else ():
+        setattr(p, name, [O.w4_dequantize(*O.w4_quantize(x)) for x in getattr(p, name)])
     hq, hkv, hd = m.n_q_heads, m.n_kv_heads, m.head_dim
     pos, slots, T = O.positions(prefix, cu), O.slot_mapping(prefix, cu, tables, 16), len(ids)
     h, stored = O.embed(p.embed, ids), []
@@ -559,23 +579,24 @@ def _layers(A, kv):
 
 
 @pytest.mark.parametrize("name,steps,norms,softcap,kv8", [
-    ("tiny", 32, True, 30.0, True), ("tiny", 1, True, 0.0, True), ("tiny", 3, False, 0.0, True), ("router", 5, True, 20.0, True),
+    ("tiny", 32, True, 30.0, True), ("tiny 4-bit", 33, True, 0.0, True), ("tiny 4-bit", 2, False, 20.0, True), ("tiny", 1, True, 0.0, True), ("tiny", 3, False, 0.0, True), ("router", 5, True, 20.0, True),
     ("router", 1, False, 30.0, True), ("tiny", 2, True, 10.0, False), ("tiny", 40, False, 25.0, False)])
 def test_prompts_enter_the_cache_and_steps_are_scored_against_them(A, name, steps, norms, softcap, kv8):
     """arb_prefill of whole prompts, then arb_score_steps of a drafted step on the same cache: the cache is what the oracle stores
     up to its rounding, and the hidden states and scores are the oracle's over that cache."""
     from helpers import HIDDEN_TOL, SCORE_TOL, rel_err
     from dataclasses import replace
-    shape = W.TINY if name == "tiny" else replace(W.ROUTER_1P5B, n_layers=2, vocab=4096)
+    four_bit = name.endswith("4-bit")
+    shape = W.TINY if name.startswith("tiny") else replace(W.ROUTER_1P5B, n_layers=2, vocab=4096)
     w = W.Workload("kv8", shape, 3, (40, 230), ("fixed", steps, steps), "shuffled", "prefill", 0.0, ("const", 0.0), 777)
-    batch, weights, gains, model, kv, db = _forward_session(A, w, 3, softcap, norms, kv8)
+    batch, weights, gains, model, kv, db = _forward_session(A, w, 3, softcap, norms, kv8, four_bit)
     prompts = H().prompt_batch(w, batch)
     A.arb_prefill(model, kv, prompts)
     ids = W.prompt_token_ids(w, batch)
     cu = np.concatenate([[0], np.cumsum(batch.prefix_lens)]).astype(np.int32)
     rounding = 2.0 ** -4 if kv8 else U
     def check(ids, prefix, cu):
-        y, stored, slots = _oracle_forward(w, weights, gains, softcap, _layers(A, kv), ids, prefix, cu, batch.block_tables)
+        y, stored, slots = _oracle_forward(w, weights, gains, softcap, _layers(A, kv), ids, prefix, cu, batch.block_tables, four_bit)
         for layer, pair in zip(_layers(A, kv), stored):
             for got, want in zip(values(layer), pair):
                 g = got.cpu().numpy()[slots // 16, :, slots % 16]
