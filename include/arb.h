@@ -15,8 +15,9 @@
  *  - "device" pointers are HIP device memory on the current device; "host"
  *    pointers are ordinary host memory.  The caller owns every buffer, including
  *    the KV pool and the workspace; the library allocates nothing in the hot
- *    calls (arb_prefill, arb_score_steps, arb_route and the arb_stage_* calls),
- *    never synchronises the device and never reads results back.
+ *    calls (arb_prefill, arb_score_steps, arb_route, the arb_stage_* calls, their
+ *    *_kv8 forms and arb_kv8_pack / arb_kv8_unpack), never synchronises the device
+ *    and never reads results back.
  *  - All work is enqueued on `stream` (a hipStream_t passed as void*; NULL is the
  *    default stream).  Outputs are valid once the caller has synchronised it.
  *  - Every call returns an arb_status; nothing throws or aborts across the ABI.
@@ -367,7 +368,9 @@ arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_
                                size_t ws_bytes, void *stream);
 
 /* Append-attention of one layer over a cache of either type, with softcap as in arb_model_set_softcap (the argument counts, not the
- * model's).  The other arguments are those of arb_stage_attention, of which this is the general form. */
+ * model's).  The other arguments are those of arb_stage_attention, of which this is the general form; without a cap and over bf16
+ * pools the results are its results.  A value of a bf16 pool that is not finite may reach every row of its step, also those that do
+ * not see its position (0 * NaN); the 8-bit format keeps it from them. */
 arb_status arb_stage_attention_kv(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
                                   const arb_kv_layer *kv, float softcap, const arb_batch *batch, void *out, void *ws,
                                   size_t ws_bytes, void *stream);
