@@ -239,7 +239,7 @@ extern "C" size_t arb_workspace_bytes(const arb_model *m, int32_t max_batch, int
   // calls of few rows per sequence and kv head (only those have tokens enough for nothing else) cut a context into up to one part more
   const long long few_tokens = (long long)max_batch * (kFewRows / G);
   const int few = few_tokens < max_total_tokens ? (int)few_tokens : max_total_tokens;
-  const size_t few_bytes = attention_ws_bytes(attention_few_parts_cap(max_ctx), 0, few, m->cfg.n_q_heads, m->cfg.head_dim);
+  const size_t few_bytes = attention_few_ws_bytes(attention_few_parts_cap(max_ctx), few, m->cfg.n_q_heads, m->cfg.head_dim);
   return carve(m->cfg, max_total_tokens, splits, items, nullptr, few_bytes).total;
 }
 
@@ -336,15 +336,16 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
   const bool few_rows = attention_few_takes(attn_cache(kv.layer(l0), m->softcap), c.head_dim, max_rows);
   FewPlan few_plan{};
   if (few_rows) few_plan = plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows, kv.kv8);
-  AttnPlan plan = few_rows ? AttnPlan{few_plan.per * ATTN_KT, few_plan.parts, 1, 0}
+  const size_t few_bytes = few_rows ? attention_few_ws_bytes(few_plan.parts, T, c.n_q_heads, c.head_dim) : 0;
+  AttnPlan plan = few_rows ? AttnPlan{ATTN_KT, 1, 1, 0}    // (no splits of the other kernel)
                            : plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   // the attention part is sized by this call's own split count (never above what arb_workspace_bytes assumed)
-  Workspace w = carve(c, T, plan.max_splits, plan.n_items, ws);
+  Workspace w = carve(c, T, plan.max_splits, plan.n_items, ws, few_bytes);
   // Scratch that has no room for the attention work list (the static buffer's size does not follow from the batch) is used
   // without one: the workgroups find their work themselves, and the results are the same.
   if (ws_bytes < w.total) {
     plan.n_items = 0;
-    w = carve(c, T, plan.max_splits, 0, ws);
+    w = carve(c, T, plan.max_splits, 0, ws, few_bytes);
   }
   if (ws_is_static && ws_bytes < w.total)
     return arb_fail(ARB_ECAPACITY, "arb_score_steps_noalloc: this batch needs %zu bytes of scratch but the static buffer "
@@ -818,7 +819,7 @@ extern "C" arb_status arb_stage_attention_kv(const arb_model *m, const void *q, 
   if (!kv) return arb_fail(ARB_EINVAL, "%s: null kv", name);
   if (arb_status s = check_layer(*kv, name)) return s;
   if (arb_status s = check_softcap(softcap, name)) return s;
-  if (!aligned16(q) || !aligned16(out)) return arb_fail(ARB_EINVAL, "%s: q and out are aligned to 16 bytes", name);
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return arb_fail(ARB_EINVAL, "%s: q, out and ws are aligned to 16 bytes", name);
   return stage_attention(name, m, q, q_row_stride, q_scaled, attn_cache(*kv, softcap), batch, out, ws, ws_bytes, stream);
 }
 

@@ -624,7 +624,7 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
 
 // Workspace: partial results [splits, T, Hq, hd] bf16 and their (m, l) fp32 (none with a single split), the splits of every
 // token, the work list (none with n_items == 0).
-size_t attention_part_bytes(int max_splits, int T, int Hq, int hd) {
+static size_t part_acc_bytes(int max_splits, int T, int Hq, int hd) {
   return max_splits > 1 ? align_up((size_t)max_splits * T * Hq * hd * sizeof(bf16), 256) : 0;
 }
 static size_t part_ml_bytes(int max_splits, int T, int Hq) {
@@ -632,12 +632,12 @@ static size_t part_ml_bytes(int max_splits, int T, int Hq) {
 }
 
 size_t attention_ws_bytes(int max_splits, size_t n_items, int total_tokens, int n_q_heads, int head_dim) {
-  return attention_part_bytes(max_splits, total_tokens, n_q_heads, head_dim) + part_ml_bytes(max_splits, total_tokens, n_q_heads) +
+  return part_acc_bytes(max_splits, total_tokens, n_q_heads, head_dim) + part_ml_bytes(max_splits, total_tokens, n_q_heads) +
          align_up((size_t)total_tokens * sizeof(int32_t), 256) + align_up(n_items * sizeof(AttnItem), 256);
 }
 
 AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int n_q_heads, int head_dim) {
-  char *p = (char *)ws + attention_part_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim) +
+  char *p = (char *)ws + part_acc_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim) +
             part_ml_bytes(plan.max_splits, total_tokens, n_q_heads);
   return AttnLists{plan.n_items > 0 ? (AttnItem *)(p + align_up((size_t)total_tokens * sizeof(int32_t), 256)) : nullptr, (int32_t *)p};
 }
@@ -654,7 +654,7 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
     return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
   const int n_items = listed ? plan.n_items : batch * plan.max_splits * n_kv_heads * plan.max_qtiles;
   bf16 *part_acc = (bf16 *)ws;
-  float *part_ml = (float *)((char *)ws + attention_part_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim));
+  float *part_ml = (float *)((char *)ws + part_acc_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim));
   const AttnLists lists = split || listed ? attention_lists(ws, plan, total_tokens, n_q_heads, head_dim) : AttnLists{};
   // Capped scores: the kernel's scale is what the exponential of the tanh takes, 2 log2(e) / cap per unit of the logit.
   const bool kv8 = cache.k_scale != nullptr, capped = cache.softcap > 0.f;

@@ -37,8 +37,8 @@ struct FewArgs {
   const int32_t *tables, *prefix_lens, *cu;
   int batch, max_blocks, max_splits, per, in_a_row, T, Hq, Hkv;
   float scale, cap_out;                      // scale: score -> logit in log2 units, or (CAP) -> the exponent of the tanh
-  bf16 *out, *part_acc;
-  float *part_ml;
+  bf16 *out;
+  float *part_acc, *part_ml;                 // fp32 throughout: few rows make little of it, and a rounding to bf16 would be as large as the result's own
 };
 
 // Word i of an array that no kernel of the launch writes, i the same for the wave: a scalar load.
@@ -390,13 +390,15 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 && KV8 ? 4 : 2) void atten
         }
       }
       const float inv = l != 0.f ? 1.0f / l : 0.f;           // NaN stays NaN; a row without visible keys in this part: 0
-      bf16x8 r;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) r[e] = (bf16)(acc[e] * inv);
       if (entire) {
+        bf16x8 r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = (bf16)(acc[e] * inv);
         *(bf16x8 *)(a.out + idx * HD + piece * 8) = r;
       } else {
-        *(bf16x8 *)(a.part_acc + ((size_t)part * a.T * a.Hq + idx) * HD + piece * 8) = r;
+        float *dst = a.part_acc + ((size_t)part * a.T * a.Hq + idx) * HD + piece * 8;
+        *(f32x4 *)dst = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        *(f32x4 *)(dst + 4) = f32x4{acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv};
         if (piece == 0) {
           float *ml = a.part_ml + ((size_t)part * a.T * a.Hq + idx) * 2;
           ml[0] = m;
@@ -470,6 +472,13 @@ static int most_parts(int n, int per) { return (n + per - 2) / per + 1; }
 
 int attention_few_parts_cap(int max_ctx) { return attention_splits_cap(max_ctx) + 1; }
 
+// Partial results [parts, T, Hq, hd] and their (m, l), fp32; none with one part.
+static size_t few_acc_bytes(int parts, int T, int Hq, int hd) { return align_up((size_t)parts * T * Hq * hd * sizeof(float), 256); }
+size_t attention_few_ws_bytes(int parts, int total_tokens, int n_q_heads, int head_dim) {
+  if (parts <= 1) return 0;
+  return few_acc_bytes(parts, total_tokens, n_q_heads, head_dim) + align_up((size_t)parts * total_tokens * n_q_heads * 2 * sizeof(float), 256);
+}
+
 FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t *cu_host, int n_kv_heads, int head_dim, int max_rows, bool kv8) {
   auto tiles = [&](int b) { return ceil_div(prefix_host[b] + cu_host[b + 1] - cu_host[b], KT); };
   long long total = 0;
@@ -512,7 +521,7 @@ arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache
                                 const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled) {
   if (batch == 0 || total_tokens == 0) return ARB_OK;
   const bool split = plan.parts > 1, capped = cache.softcap > 0.f;
-  const size_t need = attention_ws_bytes(plan.parts, 0, total_tokens, n_q_heads, head_dim);
+  const size_t need = attention_few_ws_bytes(plan.parts, total_tokens, n_q_heads, head_dim);
   if (split && (!ws || ws_bytes < need)) return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
   if (plan.tiles + plan.per > 0x7fffffffLL || plan.groups >= 1 << 24)
     return arb_fail(ARB_EUNSUPPORTED, "attention: %lld tiles of keys in one call", plan.tiles);
@@ -521,8 +530,8 @@ arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache
             block_tables, prefix_lens, cu_step_lens, batch, max_blocks_per_seq, plan.parts, plan.per, plan.in_a_row, total_tokens, n_q_heads,
             n_kv_heads, capped ? 2.0f * to_log2 / cache.softcap : to_log2, capped ? 1.44269504f * cache.softcap : 0.f, out, nullptr, nullptr};
   if (split) {
-    a.part_acc = (bf16 *)ws;
-    a.part_ml = (float *)((char *)ws + attention_part_bytes(plan.parts, total_tokens, n_q_heads, head_dim));
+    a.part_acc = (float *)ws;
+    a.part_ml = (float *)((char *)ws + few_acc_bytes(plan.parts, total_tokens, n_q_heads, head_dim));
   }
   const dim3 grid = plan.in_a_row ? dim3((unsigned)plan.groups) : dim3(n_kv_heads, plan.parts, batch), block(256);
 #define ARB_FEW(HD, NQ)                                                                                                     \

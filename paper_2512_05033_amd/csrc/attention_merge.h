@@ -18,22 +18,24 @@ struct SplitSum {
   // Splits first, first + step, ... below n_splits, eight at a time: all their loads go out together (a loop over a run-time count
   // waits for each before it asks for the next), then they are combined under their common maximum; groups of eight are
   // chained by the usual online rescaling.
-  template <int HD>
-  __device__ __forceinline__ void add(const bf16 *__restrict__ part_acc, const float *__restrict__ part_ml, size_t stride,
+  // Part: bf16 or float.
+  template <int HD, typename Part>
+  __device__ __forceinline__ void add(const Part *__restrict__ part_acc, const float *__restrict__ part_ml, size_t stride,
                                       size_t idx, int piece, int first, int step, int n_splits) {
+    typedef Part part8 __attribute__((ext_vector_type(8)));
     for (int s0 = first; s0 < n_splits; s0 += 8 * step) {
       float2 ml[8];
-      bf16x8 v[8];
+      part8 v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int s = s0 + j * step;
         if (s < n_splits) {
           ml[j] = *(const float2 *)(part_ml + (s * stride + idx) * 2);
-          v[j] = *(const bf16x8 *)(part_acc + (s * stride + idx) * HD + piece * 8);
+          v[j] = *(const part8 *)(part_acc + (s * stride + idx) * HD + piece * 8);
         } else {
           ml[j] = float2{-INFINITY, 0.f};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[j][e] = (bf16)0.f;
+          for (int e = 0; e < 8; ++e) v[j][e] = (Part)0.f;
         }
       }
       float m_new = m;

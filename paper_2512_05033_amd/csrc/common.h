@@ -166,10 +166,7 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
                             const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled,
                             bool count_splits = false);   // count_splits: no launch_token_meta has written the tokens' splits
-size_t attention_part_bytes(int max_splits, int total_tokens, int n_q_heads, int head_dim);   // of the partial results, in front of their (m, l)
-
-// attention_few.hip: few query rows (step tokens x query heads of one kv head) over an 8-bit cache, or capped.  The workspace is
-// attention_ws_bytes of `parts` splits without a work list.
+// attention_few.hip: few query rows (step tokens x query heads of one kv head) over an 8-bit cache, or capped.
 struct FewPlan {
   int per;                 // 64-key tiles of a workgroup, at most
   int in_a_row;            // whether a workgroup's tiles run on from one (sequence, kv head) to the next; otherwise each is cut evenly
@@ -177,6 +174,7 @@ struct FewPlan {
   long long groups, tiles; // workgroups, and tiles of the batch
 };
 bool attention_few_takes(const AttnCache &cache, int head_dim, int max_rows);
+size_t attention_few_ws_bytes(int parts, int total_tokens, int n_q_heads, int head_dim);
 int attention_few_parts_cap(int max_ctx);   // largest `parts` for contexts <= max_ctx
 FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t *cu_host, int n_kv_heads, int head_dim, int max_rows, bool kv8);
 arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache &cache, const int32_t *block_tables,

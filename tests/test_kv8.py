@@ -148,6 +148,7 @@ def test_single_stages_are_checked_on_the_host(lib):
     assert attend(full, stride=width - 8) == B.ARB_EINVAL and attend(full, stride=width + 4) == B.ARB_EINVAL
     long = _batch(B, prefix=(5000, 20), blocks=400)
     assert attend(full, batch=long, ws_bytes=64) == B.ARB_ECAPACITY and attend(full, batch=long, ws=None) == B.ARB_ECAPACITY
+    assert attend(full, ws=P + 8) == B.ARB_EINVAL and attend(full, out=P + 2) == B.ARB_EINVAL
     assert append(full, qkv=None) == B.ARB_EINVAL and append(full, q_out=P + 2) == B.ARB_EINVAL
     assert append(full, g_q=P + 8) == B.ARB_EINVAL and append(full, qkv=P + 8) == B.ARB_EINVAL
     lib.arb_model_destroy(h)
