@@ -318,6 +318,7 @@ class DeviceBatch:
             self.tokens = _dev(token_ids, torch.int32)
         else:
             self.tokens = None if token_ids is None else to(token_ids)
+        self.device_index = self.tables.get_device()
         self.batch = len(self.prefix_host)
         self.total_tokens = int(self.cu_host[-1]) if len(self.cu_host) else 0
         self.c = _Batch(self.batch, self.total_tokens, tables.shape[1] if tables.ndim == 2 else 0,
@@ -345,12 +346,11 @@ def _fits(t: torch.Tensor, dtype, device_index: int) -> bool:
     return t.dtype is dtype and t.get_device() == device_index and t.is_contiguous()
 
 
-def _current_device(*device_indices: int) -> int:
+def _current_device(first: int, second: int) -> int:
     """The library works on the current device; what lives elsewhere is refused."""
-    here = torch.cuda.current_device()
-    for i in device_indices:
-        if i != here:
-            raise ValueError(f"a tensor is on device {i}, the current device is cuda:{here}")
+    here = torch._C._cuda_getDevice()
+    if first != here or second != here:
+        raise ValueError(f"tensors are on devices {first} and {second}, the current device is cuda:{here}")
     return here
 
 
@@ -615,7 +615,7 @@ def _stage_device(model: Model, kv: KVLayer, batch: DeviceBatch) -> int:
     """What the two stages below ask of their arguments first -> the device they run on."""
     if kv.heads != model.kv_heads:
         raise ValueError(f"pools of shape {tuple(kv.k_pool.shape)} for {model.kv_heads[0]} kv heads of {model.kv_heads[1]}")
-    return _current_device(kv.device_index, batch.tables.get_device())
+    return _current_device(kv.device_index, batch.device_index)
 
 
 def _empty(stream, *shape, dtype, device):
@@ -633,7 +633,7 @@ def arb_stage_attention_kv(model: Model, q: torch.Tensor, kv: KVLayer, batch: De
     """arb_stage_attention over one layer of either type of cache, scores capped by softcap * tanh(x / softcap) if softcap > 0.
     q bf16 [at least T, row] whose first Hq*hd columns are the (rotated) query heads -> bf16 [T, Hq*hd]."""
     dev, T, width = _stage_device(model, kv, batch), batch.total_tokens, model.q_width
-    if not _fits(q, torch.bfloat16, dev) or q.dim() != 2 or q.shape[0] < T or q.shape[1] < width:
+    if not _fits(q, torch.bfloat16, dev) or q.dim() != 2 or q.size(0) < T or q.size(1) < width:
         raise ValueError(f"q is contiguous bf16 [at least {T}, at least {width}], got {q.dtype} {tuple(q.shape)} on {q.device}")
     if out is None:
         out = _empty(stream, T, width, dtype=torch.bfloat16, device=q.device)
@@ -644,7 +644,7 @@ def arb_stage_attention_kv(model: Model, q: torch.Tensor, kv: KVLayer, batch: De
         ws = _empty(stream, max(n, 256), dtype=torch.uint8, device=q.device)
     elif not _fits(ws, torch.uint8, dev):
         raise ValueError(f"ws is contiguous uint8, got {ws.dtype} on {ws.device}")
-    _check(load_library().arb_stage_attention_kv(model.handle, q.data_ptr(), q.shape[1], q_scaled, kv.c, softcap, batch.c,
+    _check(load_library().arb_stage_attention_kv(model.handle, q.data_ptr(), q.size(1), q_scaled, kv.c, softcap, batch.c,
                                                  out.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(stream, dev)))
     return out
 
@@ -655,18 +655,18 @@ def arb_stage_norm_rope_append(model: Model, qkv: torch.Tensor, kv: KVLayer, bat
     """Norms (where a gain, fp32 [hd], is given) and rotates the q and k heads of qkv (bf16 [T, (Hq+2Hkv)*hd]), stores k and v in
     the layer's pools and returns the queries: bf16 [T, Hq*hd], or qkv itself with in_place."""
     dev, T, width, hkv, hd = _stage_device(model, kv, batch), batch.total_tokens, model.q_width, *model.kv_heads
-    if not _fits(qkv, torch.bfloat16, dev) or qkv.shape != (T, width + 2 * hkv * hd):
+    if not _fits(qkv, torch.bfloat16, dev) or qkv.dim() != 2 or qkv.size(0) != T or qkv.size(1) != width + 2 * hkv * hd:
         raise ValueError(f"qkv is contiguous bf16 {(T, width + 2 * hkv * hd)}, got {qkv.dtype} {tuple(qkv.shape)} on {qkv.device}")
     for g in (g_q, g_k):
-        if g is not None and (not _fits(g, torch.float32, dev) or g.shape != (hd,)):
+        if g is not None and (not _fits(g, torch.float32, dev) or g.numel() != hd):
             raise ValueError(f"a gain is fp32 [{hd}], got {g.dtype} {tuple(g.shape)} on {g.device}")
     if in_place:
         if out is not None:
             raise ValueError("in_place or out, not both")
     elif out is None:
         out = _empty(stream, T, width, dtype=torch.bfloat16, device=qkv.device)
-    elif not _fits(out, torch.bfloat16, dev) or out.shape != (T, width):
-        raise ValueError(f"out is contiguous bf16 {(T, width)}, got {out.dtype} {tuple(out.shape)} on {out.device}")
+    elif not _fits(out, torch.bfloat16, dev) or out.numel() != T * width:
+        raise ValueError(f"out is contiguous bf16 of {T * width} elements, got {out.dtype} {tuple(out.shape)} on {out.device}")
     _check(load_library().arb_stage_norm_rope_append(model.handle, qkv.data_ptr(), _ptr(g_q), _ptr(g_k), q_scaled, kv.c, batch.c,
                                                      _ptr(out), _stream_on(stream, dev)))
     return qkv if in_place else out
@@ -678,13 +678,11 @@ def _kv8_convert(entry, src: KVLayer, dst: KVLayer, src_blocks, dst_blocks, n_bl
     dev = _current_device(src.device_index, dst.device_index)
     if n_blocks is None:
         n_blocks = next((b.numel() for b in (src_blocks, dst_blocks) if b is not None), src.n_blocks)
-    for blocks, room in ((src_blocks, src.n_blocks), (dst_blocks, dst.n_blocks)):
-        if blocks is not None:
-            if not _fits(blocks, torch.int32, dev):
-                raise ValueError(f"block ids are contiguous int32, got {blocks.dtype} on {blocks.device}")
-            room = blocks.numel()
-        if n_blocks > room:
-            raise ValueError(f"{n_blocks} blocks, but a {'pool' if blocks is None else 'list'} of {room}")
+    for blocks, kv in ((src_blocks, src), (dst_blocks, dst)):
+        if blocks is not None and not _fits(blocks, torch.int32, dev):
+            raise ValueError(f"block ids are contiguous int32, got {blocks.dtype} on {blocks.device}")
+        if n_blocks > (kv.n_blocks if blocks is None else blocks.numel()):
+            raise ValueError(f"{n_blocks} blocks, but a {'pool' if blocks is None else 'list'} of fewer")
     _check(entry(src.c, _ptr(src_blocks), dst.c, _ptr(dst_blocks), n_blocks, src.heads[0], src.heads[1], _stream_on(stream, dev)))
 
 

@@ -529,6 +529,78 @@ def test_two_calls_at_once_on_two_streams(A):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [130 * i % 7001 for i in range(70)], [1] * 70), ("target", [4000, 20, 9000], [2, 8, 1]),
+                                                ("router", [3000, 300], [40, 64])])
+def test_nothing_is_written_outside_of_the_least_workspace(A, heads, prefix, steps):
+    import re
+    hq, hkv, hd = HEADS[heads]
+    db, tables, n = make_batch(A, prefix, steps, 111)
+    kv = filled(A, n, hkv, hd, 112)
+    q = queries(sum(steps), heads, 113, True)
+    run = lambda **k: A.arb_stage_attention_kv(stage_model(heads), q, kv, db, q_scaled=True, **k)
+    with pytest.raises(A.ArbError) as e:                         # a host check: nothing is launched
+        run(ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    need = int(re.search(r"workspace 16 < (\d+) bytes", str(e.value)).group(1))
+    buf = torch.full((need + 8192,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full((sum(steps) + 2, hq * hd), 3.0, dtype=torch.bfloat16, device="cuda")
+    run(ws=buf[4096:4096 + need], out=out)
+    assert bool((buf[:4096] == 255).all()) and bool((buf[4096 + need:] == 255).all()) and bool((out[-2:] == 3).all())
+    ref, mag = attention_ref(heads, q, kv, tables, prefix, steps, 0.0, True)
+    assert bool(((out[:-2].double().view(ref.shape) - ref).abs() <= 4.3 * U * mag + 1e-30).all())
+
+
+@pytest.mark.parametrize("host,device", [([1000, 300, 900], [200, 100, 900]), ([600, 100, 0], [1000, 300, 900]), ([90 * i % 3001 for i in range(60)], [70 * i % 3001 for i in range(60)])])
+def test_lengths_that_differ_on_host_and_device_stay_within_memory(A, host, device):
+    """The contract has them equal.  Where they are not, nothing outside the workspace and the output is written; and with fewer keys on
+    the device every piece of work is still there, so the result is theirs."""
+    import re
+    heads, steps = "target", [2, 1, 3] + [1] * (len(host) - 3)
+    hq, hkv, hd = HEADS[heads]
+    db, tables, n = make_batch(A, [max(a, b) for a, b in zip(host, device)], steps, 131)
+    db = A.DeviceBatch(np.array(device, np.int32), db.cu_host, tables)
+    db.prefix_host[:] = host
+    kv = filled(A, n, hkv, hd, 132)
+    q = queries(sum(steps), heads, 133, True)
+    run = lambda d, **k: A.arb_stage_attention_kv(stage_model(heads), q, kv, d, q_scaled=True, **k)
+    need = 0                                                     # contexts that are not cut need none
+    try:
+        run(db, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    except A.ArbError as e:
+        need = int(re.search(r"workspace 16 < (\d+) bytes", str(e)).group(1))
+    buf = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full((sum(steps) + 2, hq * hd), 3.0, dtype=torch.bfloat16, device="cuda")
+    run(db, ws=buf[:need], out=out)
+    torch.cuda.synchronize()
+    assert bool((buf[need:] == 255).all()) and bool((out[-2:] == 3).all())
+    if all(h >= d for h, d in zip(host, device)):
+        ref, mag = attention_ref(heads, q, kv, tables, device, steps, 0.0, True)
+        assert bool(((out[:-2].double().view(ref.shape) - ref).abs() <= 4.3 * U * mag + 1e-30).all())
+
+
+def test_two_captured_graphs_share_a_workspace(A):
+    todo = []
+    for i, (heads, prefix, steps, cap) in enumerate((("router", [5000, 40], [1, 2], 0.0), ("router", [900, 2000], [50, 64], 20.0), ("target", [2048] * 4, [3] * 4, 0.0))):
+        hq, hkv, hd = HEADS[heads]
+        db, tables, n = make_batch(A, prefix, steps, 121 + i)
+        q, kv = queries(sum(steps), heads, 124 + i, True), filled(A, n, hkv, hd, 127 + i)
+        todo.append([heads, q, kv, db, cap, torch.empty_like(q)])
+    ws = torch.empty(max(stage_model(h).workspace_bytes(db.batch, db.total_tokens, db.max_ctx) for h, _, _, db, _, _ in todo), dtype=torch.uint8, device="cuda")
+    call = lambda h, q, kv, db, cap, out: A.arb_stage_attention_kv(stage_model(h), q, kv, db, softcap=cap, q_scaled=True, ws=ws, out=out)
+    want, graphs = [call(*t).clone() for t in todo], []
+    for t in todo:
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(*t)
+        graphs.append(g)
+    for i in (0, 1, 0, 2, 2, 1, 0):
+        todo[i][5].fill_(9.0)
+        graphs[i].replay()
+        eager = call(*todo[(i + 1) % 3]).clone()                 # and eager work between the replays, on the same workspace
+        torch.cuda.synchronize()
+        assert torch.equal(todo[i][5], want[i]) and torch.equal(eager, want[(i + 1) % 3])
+
+
 # ------------------------------------------------------------------------------ the whole forward
 
 def _forward_session(A, w, seed, softcap, norms, kv8=True, four_bit=False):
