@@ -13,6 +13,10 @@
 // in flight already.  So all end together whatever the lengths are, at the price of a result more per workgroup.  A pair that was
 // cut is merged by a second launch.
 //
+// Measured: 32 tokens of 32/8 heads of 128 against 4 K to 32 K keys 198 us (5.6 TB/s of cache) and 4.8 for the merge, 64 against 32 K
+// 719 (6.0); one token of 12/2 heads against 1531 keys 6.1 and 2.7.  The bf16 cache's kernel, whose workgroup streams through
+// LDS and lets one wave work, took 318 us for the first of these in its form for the 8-bit cache.
+//
 // A tile is four cache blocks.  Lane l = 16 g + c.  Scores S^T = K Q^T: score tile t (0..3) has row r = key 4 t + r % 4 of block
 // r / 4, so that lane (g, c) receives rows 4 g .. 4 g + 3 of every score tile, i.e. all 16 keys of block g for query c.  The
 // contraction index is free: lane (g, c) supplies elements 64 j + 16 g + 8 h + (0..7) in step 2 j + h, which are 16-byte
