@@ -299,6 +299,7 @@ CASES = [
     ("router", [0], [1]), ("router", [1531], [1]), ("target", [0, 1, 15, 16, 63, 64, 65, 127], [1] * 8),
     ("multi", [4000, 17, 900], [1, 2, 1]), ("single", [300, 40, 1000], [16, 5, 9]), ("tiny", [5, 0, 1700, 64], [1, 9, 3, 8]),
     ("router", [2048, 100, 0], [5, 3, 4]), ("target", [700, 64], [8, 7]),
+    ("target", [700, 64, 5], [9, 16, 1]), ("router", [2048, 100, 63], [10, 3, 6]), ("tiny", [300, 5], [32, 17]), ("multi", [900, 0], [8, 5]), ("single", [40, 500], [64, 33]),
     ("router", [300, 77, 1000, 0, 2048], [5, 64, 33, 20, 1]), ("target", [4096, 15], [64, 129]), ("tiny", [512, 3, 130], [32, 64, 200]),
     ("tiny", [0], [4300]), ("multi", [200], [300]), ("single", [100, 3], [150, 1]),
 ]
@@ -314,7 +315,8 @@ def test_attention(A, heads, prefix, steps, cap, q_scaled, kv8):
     check_attention(A, heads, kv, prefix, steps, 23, db, tables, cap, q_scaled, extra=0 if q_scaled else 64)
 
 
-@pytest.mark.parametrize("heads,prefix,steps", [("router", [9000, 30000], [1, 1]), ("target", [32767], [2]), ("tiny", [20000, 3], [1, 8]), ("multi", [16383], [16])])
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [9000, 30000], [1, 1]), ("target", [32767], [2]), ("tiny", [20000, 3], [1, 8]), ("multi", [16383], [16]), ("target", [9000, 20000], [16, 9]),
+                                                ("single", [7000], [50])])
 @pytest.mark.parametrize("cap", [0.0, 30.0])
 def test_attention_over_long_contexts(A, heads, prefix, steps, cap):
     hq, hkv, hd = HEADS[heads]
@@ -339,7 +341,7 @@ def test_attention_of_few_rows_however_it_is_split(A, heads, prefix, steps, in_a
     check_attention(A, heads, kv, prefix, steps, 37, db, tables, cap, True)
 
 
-@pytest.mark.parametrize("heads,prefix,steps", [("router", [700, 64], [2, 1]), ("target", [1000], [40]), ("tiny", [333], [7])])
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [700, 64], [2, 1]), ("target", [1000], [40]), ("tiny", [333], [7]), ("target", [650], [13])])
 @pytest.mark.parametrize("cap", [0.0, 15.0])
 def test_attention_with_scores_that_jump(A, heads, prefix, steps, cap):
     """Queries eight times as large and planted keys: the running maximum moves late, and one key takes nearly all."""
@@ -373,7 +375,7 @@ def test_long_steps_are_the_attention_over_the_unpacked_cache_bit_for_bit(A, hea
         assert torch.equal(run(plain), A.arb_stage_attention(stage_model(heads), q, plain.k_pool, plain.v_pool, db, q_scaled=True))
 
 
-@pytest.mark.parametrize("heads,prefix,steps", [("router", [13, 40, 64], [1, 2, 1]), ("target", [5], [60]), ("tiny", [63, 1], [3, 1]), ("router", [600], [1])])
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [13, 40, 64], [1, 2, 1]), ("target", [5], [60]), ("tiny", [63, 1], [3, 1]), ("router", [600], [1]), ("target", [70, 1], [11, 2])])
 @pytest.mark.parametrize("fill,kv8,cap", [(0x7f, True, 0.0), (0xff, True, 9.0), (0xff, False, 9.0)])
 def test_slots_past_the_context_may_hold_anything(A, heads, prefix, steps, fill, kv8, cap):
     hq, hkv, hd = HEADS[heads]
@@ -397,7 +399,7 @@ def test_slots_past_the_context_may_hold_anything(A, heads, prefix, steps, fill,
     assert bool(torch.isfinite(run(full)).all()) and torch.equal(run(kv), run(full))
 
 
-@pytest.mark.parametrize("steps", [4, 40])
+@pytest.mark.parametrize("steps", [4, 9, 40])
 @pytest.mark.parametrize("bad", ["nan key", "infinite value"])
 def test_a_position_that_is_not_finite_is_seen_by_those_that_see_it(A, steps, bad):
     """Append a step whose token 2 is broken in kv head 1, attend: rows before it as without it, rows from it on NaN, head 0 untouched."""
