@@ -393,7 +393,7 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 && KV8 ? 4 : 2) void atten
           acc[4 + e] += f * x1[e];
         }
       }
-      const float inv = l != 0.f ? 1.0f / l : 0.f;           // NaN stays NaN; a row without visible keys in this part: 0
+      const float inv = entire || l != 0.f ? 1.0f / l : 0.f;   // NaN stays NaN; a row without visible keys in this part: 0
       if (entire) {
         bf16x8 r;
 #pragma unroll

@@ -41,15 +41,15 @@ struct SplitSum {
       float m_new = m;
 #pragma unroll
       for (int j = 0; j < 8; ++j) m_new = fmaxf(m_new, ml[j].x);
-      if (m_new == -INFINITY) continue;                    // no key of these splits is visible to the row
-      const float keep = exp2f(m - m_new);                 // m = -inf: 0
+      // No key of any split so far visible to the row, or NaN all of them: the weights are 0 and keep a NaN.
+      const float ref = m_new == -INFINITY ? 0.f : m_new, keep = exp2f(m - ref);   // m = -inf: 0
       m = m_new;
       l *= keep;
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] *= keep;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float w = exp2f(ml[j].x - m_new) * ml[j].y;  // a split without visible keys: exp2(-inf) * 0 = 0
+        const float w = exp2f(ml[j].x - ref) * ml[j].y;  // a split without visible keys: exp2(-inf) * 0 = 0
         l += w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] += w * (float)v[j][e];

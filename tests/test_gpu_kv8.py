@@ -265,19 +265,19 @@ def test_norm_rope_append_forms(A, norms, q_scaled, in_place):
 
 
 def test_append_of_many_tokens_is_that_of_few(A):
-    """From 1024 tokens on a workgroup takes four tokens: the same bits as sequence by sequence."""
+    """From 768 tokens on a lane takes eight pairs and a workgroup two tokens: the same bits as one token fewer."""
     hq, hkv, hd = HEADS["target"]
-    prefix, steps = [3, 0, 800], [500, 1, 522]
+    prefix, steps = [3, 0, 800], [500, 1, 266]
     db, tables, n = make_batch(A, prefix, steps, 5)
-    qkv = rows((1023, (hq + 2 * hkv) * hd), 6)
+    qkv = rows((767, (hq + 2 * hkv) * hd), 6)
     more = rows((1, (hq + 2 * hkv) * hd), 7)
     both, one = layer8(A, n + 1, hkv, hd), layer8(A, n + 1, hkv, hd)
     g = 1 + 0.2 * torch.randn(hd, device="cuda")
     q1 = A.arb_stage_norm_rope_append(stage_model("target"), qkv, one, db, g, g)
     t4 = np.concatenate([tables, np.full((1, tables.shape[1]), n, np.int32)])
-    db4 = A.DeviceBatch(np.array(prefix + [2], np.int32), np.array([0, 500, 501, 1023, 1024], np.int32), t4)
+    db4 = A.DeviceBatch(np.array(prefix + [2], np.int32), np.array([0, 500, 501, 767, 768], np.int32), t4)
     q4 = A.arb_stage_norm_rope_append(stage_model("target"), torch.cat([qkv, more]), both, db4, g, g)
-    assert torch.equal(q4[:1023], q1)
+    assert torch.equal(q4[:767], q1)
     for name in ("k_pool", "v_pool", "k_scale", "v_scale"):
         assert torch.equal(getattr(both, name).view(torch.uint8)[:n], getattr(one, name).view(torch.uint8)[:n])
 
@@ -420,6 +420,29 @@ def test_a_position_that_is_not_finite_is_seen_by_those_that_see_it(A, steps, ba
     good, got = outs
     assert torch.equal(got[:2], good[:2]) and torch.equal(got[:, :6], good[:, :6]) and bool(torch.isfinite(good).all())
     assert bool(torch.isnan(got[2:, 6:]).all())
+
+
+@pytest.mark.parametrize("heads,prefix,steps", [("target", 12000, 4), ("router", 20000, 1), ("tiny", 9000, 16), ("target", 9000, 40), ("router", 30000, 12)])
+@pytest.mark.parametrize("kv8,cap", [(True, 0.0), (True, 12.0), (False, 12.0), (False, 0.0)])
+def test_a_long_stretch_of_keys_that_are_not_finite(A, heads, prefix, steps, kv8, cap):
+    """The first keys of a split context are NaN, up to every fourth tile: whole parts and whole groups of parts.  Whoever sees any
+    of them gets NaN; the other sequence is as it was."""
+    hq, hkv, hd = HEADS[heads]
+    prefix, steps = [prefix, 100], [steps, 1]
+    db, tables, n = make_batch(A, prefix, steps, 81)
+    kv = filled(A, n, hkv, hd, 82, kv8)
+    q = queries(sum(steps), heads, 83, True)
+    run = lambda: A.arb_stage_attention_kv(stage_model(heads), q, kv, db, softcap=cap, q_scaled=True)
+    good = run()
+    assert bool(torch.isfinite(good).all())
+    for first in range(0, prefix[0] // 16 - 16, 16):
+        bad = torch.from_numpy(tables[0, first:first + 16].astype(np.int64)).cuda()
+        if kv8:
+            kv.k_pool.view(torch.uint8)[bad] = 0x7f
+        else:
+            kv.k_pool[bad] = float("nan")
+        got = run()
+        assert torch.equal(got[steps[0]:], good[steps[0]:]) and bool(torch.isnan(got[:steps[0]]).all()), first
 
 
 def test_blocks_beyond_32_bit_offsets(A):
@@ -654,7 +677,7 @@ def _layers(A, kv):
 
 @pytest.mark.parametrize("name,steps,norms,softcap,kv8", [
     ("tiny", 32, True, 30.0, True), ("tiny 4-bit", 33, True, 0.0, True), ("tiny 4-bit", 2, False, 20.0, True), ("tiny", 1, True, 0.0, True), ("tiny", 3, False, 0.0, True), ("router", 5, True, 20.0, True),
-    ("router", 1, False, 30.0, True), ("tiny", 2, True, 10.0, False), ("tiny", 40, False, 25.0, False)])
+    ("tiny long", 2, True, 0.0, True), ("tiny long", 3, True, 15.0, False), ("router", 1, False, 30.0, True), ("tiny", 2, True, 10.0, False), ("tiny", 40, False, 25.0, False)])
 def test_prompts_enter_the_cache_and_steps_are_scored_against_them(A, name, steps, norms, softcap, kv8):
     """arb_prefill of whole prompts, then arb_score_steps of a drafted step on the same cache: the cache is what the oracle stores
     up to its rounding, and the hidden states and scores are the oracle's over that cache."""
@@ -662,7 +685,7 @@ def test_prompts_enter_the_cache_and_steps_are_scored_against_them(A, name, step
     from dataclasses import replace
     four_bit = name.endswith("4-bit")
     shape = W.TINY if name.startswith("tiny") else replace(W.ROUTER_1P5B, n_layers=2, vocab=4096)
-    w = W.Workload("kv8", shape, 3, (40, 230), ("fixed", steps, steps), "shuffled", "prefill", 0.0, ("const", 0.0), 777)
+    w = W.Workload("kv8", shape, 3, (300, 600) if name.endswith("long") else (40, 230), ("fixed", steps, steps), "shuffled", "prefill", 0.0, ("const", 0.0), 777)
     batch, weights, gains, model, kv, db = _forward_session(A, w, 3, softcap, norms, kv8, four_bit)
     prompts = H().prompt_batch(w, batch)
     A.arb_prefill(model, kv, prompts)
