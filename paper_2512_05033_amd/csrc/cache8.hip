@@ -193,17 +193,26 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     const bool is_q = h < a.Hq;
     const float *g = is_q ? a.g_q : a.g_k;
     if (g) {
-      float sum[PAIRS / 4];                                // of every four pairs by itself, joined last: the same order for both widths
+      float f = 1.0f;
+      auto mean_square = [&] {                             // of f x
+        float sum[PAIRS / 4];                              // of every four pairs by itself, joined last: the same order for both widths
 #pragma unroll
-      for (int w = 0; w < PAIRS / 4; ++w) {
-        sum[w] = 0.f;
+        for (int w = 0; w < PAIRS / 4; ++w) {
+          sum[w] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[w] += x[4 * w + e] * x[4 * w + e];
+          for (int e = 0; e < 4; ++e) sum[w] += (f * x[4 * w + e]) * (f * x[4 * w + e]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[w] += x[PAIRS + 4 * w + e] * x[PAIRS + 4 * w + e];
-        sum[w] = row_sum<LANES>(sum[w]);
+          for (int e = 0; e < 4; ++e) sum[w] += (f * x[PAIRS + 4 * w + e]) * (f * x[PAIRS + 4 * w + e]);
+          sum[w] = row_sum<LANES>(sum[w]);
+        }
+        return (PAIRS == 8 ? sum[0] + sum[PAIRS / 4 - 1] : sum[0]) * (1.0f / HD);
+      };
+      float mean = mean_square();
+      if (mean == INFINITY) {                              // squares beyond fp32: those of 2^-64 x, and eps is nothing beside them
+        f = 0x1p-64f;
+        mean = mean_square();
       }
-      const float r = 1.0f / sqrtf((PAIRS == 8 ? sum[0] + sum[PAIRS / 4 - 1] : sum[0]) * (1.0f / HD) + a.eps);
+      const float r = f / sqrtf(mean + a.eps);
 #pragma unroll
       for (int w = 0; w < PAIRS / 4; ++w) {
         const f32x4 g0 = *(const f32x4 *)(g + t + 4 * w), g1 = *(const f32x4 *)(g + t + HALF + 4 * w);

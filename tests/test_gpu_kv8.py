@@ -293,6 +293,16 @@ def test_rows_of_zeros_and_rows_at_the_border_of_a_scale(A):
     assert sorted(kv.v_scale.unique().tolist())[0] == 27
 
 
+@pytest.mark.parametrize("tokens", [5, 800])
+def test_norms_of_rows_whose_squares_leave_fp32(A, tokens):
+    """Rows of magnitudes from 1e-30 to 1e37 are normed like any other (their squares are 0 or infinite in fp32)."""
+    hq, hkv, hd = HEADS["router"]
+    x = rows((tokens, hq + 2 * hkv, hd), 18, 1.0).float()
+    size = torch.tensor([1e-30, 1e-3, 1e18, 1e20, 1e35], device="cuda")[torch.arange(tokens, device="cuda") % 5]
+    x[:, :hq + hkv] *= size[:, None, None]
+    check_append(A, "router", [20], [tokens], True, (True, True), False, 19, qkv=x.bfloat16().view(tokens, -1))
+
+
 # ------------------------------------------------------------------------------------ attention
 
 CASES = [
