@@ -288,8 +288,8 @@ class KVCache8:
     of a KVCache."""
 
     def __init__(self, layers: List[KVLayer]):
-        if not layers or not all(l.kv8 for l in layers) or len({l.k_pool.shape for l in layers}) != 1:
-            raise ValueError("an 8-bit cache is a list of 8-bit layers of one shape")
+        if not layers or not all(l.kv8 for l in layers) or len({(l.k_pool.shape, l.device_index) for l in layers}) != 1:
+            raise ValueError("an 8-bit cache is a list of 8-bit layers of one shape on one device")
         self.layers = list(layers)
         self._tables = [_ptr_array([getattr(l, n) for l in self.layers]) for n in ("k_pool", "v_pool", "k_scale", "v_scale")]
         self.c = _KV8(*self._tables, int(layers[0].k_pool.shape[0]))
@@ -337,9 +337,16 @@ def _workspace(model: Model, batch: DeviceBatch, ws: Optional[torch.Tensor]) -> 
     return ws
 
 
-def _by_cache(kv, name: str):
-    """The library's entry for this type of cache."""
-    return getattr(load_library(), name + ("_kv8" if isinstance(kv, KVCache8) else ""))
+def _by_cache(model: Model, kv, name: str):
+    """The library's entry for this type of cache, which has to be the model's."""
+    if not isinstance(kv, KVCache8):
+        return getattr(load_library(), name)
+    if len(kv.layers) < model.cfg.n_layers or kv.layers[0].heads != model.kv_heads:
+        raise ValueError(f"{len(kv.layers)} layers of {kv.layers[0].heads[0]} kv heads of {kv.layers[0].heads[1]} for a model of "
+                         f"{model.cfg.n_layers} layers of {model.kv_heads[0]} of {model.kv_heads[1]}")
+    if kv.layers[0].device_index != model.device.index:
+        raise ValueError(f"the cache is on device {kv.layers[0].device_index}, the model on {model.device}")
+    return getattr(load_library(), name + "_kv8")
 
 
 def _fits(t: torch.Tensor, dtype, device_index: int) -> bool:
@@ -370,7 +377,7 @@ def arb_score_steps(model: Model, kv: KVCache, batch: DeviceBatch, tau: float, *
     if want_hidden and hidden is None:
         hidden = torch.empty(batch.total_tokens, model.cfg.d_model, dtype=torch.bfloat16, device=dev)
     ws = _workspace(model, batch, ws)
-    _check(_by_cache(kv, "arb_score_steps")(model.handle, C.byref(kv.c), C.byref(batch.c), float(tau), _ptr(scores),
+    _check(_by_cache(model, kv, "arb_score_steps")(model.handle, C.byref(kv.c), C.byref(batch.c), float(tau), _ptr(scores),
                                             _ptr(escalate), _ptr(hidden), ws.data_ptr(), ws.numel(), _stream(stream)))
     return scores, escalate, hidden
 
@@ -392,7 +399,7 @@ def arb_prefill(model: Model, kv: KVCache, batch: DeviceBatch, *, want_hidden: b
     if want_hidden:
         hidden = torch.empty(batch.total_tokens, model.cfg.d_model, dtype=torch.bfloat16, device=model.device)
     ws = _workspace(model, batch, ws)
-    _check(_by_cache(kv, "arb_prefill")(model.handle, C.byref(kv.c), C.byref(batch.c), _ptr(hidden), ws.data_ptr(),
+    _check(_by_cache(model, kv, "arb_prefill")(model.handle, C.byref(kv.c), C.byref(batch.c), _ptr(hidden), ws.data_ptr(),
                                         ws.numel(), _stream(stream)))
     return hidden
 
@@ -721,7 +728,7 @@ def arb_stage_layers(model: Model, kv: KVCache, batch: DeviceBatch, layer_begin:
         raise ValueError("residual stream shape")
     h_out = torch.empty_like(h_in)
     ws = _workspace(model, batch, ws)
-    _check(_by_cache(kv, "arb_stage_layers")(model.handle, C.byref(kv.c), C.byref(batch.c), layer_begin, layer_end,
+    _check(_by_cache(model, kv, "arb_stage_layers")(model.handle, C.byref(kv.c), C.byref(batch.c), layer_begin, layer_end,
                                              _ptr(h_in), _ptr(h_out), ws.data_ptr(), ws.numel(), _stream(stream)))
     return h_out
 

@@ -548,6 +548,23 @@ def test_the_binding_refuses_what_does_not_fit(A):
             call()
 
 
+def test_a_cache_of_fewer_layers_or_other_heads_is_refused(A):
+    shape = W.TINY
+    w = W.Workload("kv8", shape, 2, (20, 40), ("fixed", 2, 2), "shuffled", "prefill", 0.0, ("const", 0.0), 779)
+    batch, weights, gains, model, kv, db = _forward_session(A, w, 5, 0.0, False)
+    fewer = A.KVCache8(kv.layers[:-1])
+    other = A.KVCache8.empty(shape.n_layers, batch.n_blocks, shape.n_kv_heads, 128 if shape.head_dim == 64 else 64)
+    heads = A.KVCache8.empty(shape.n_layers, batch.n_blocks, shape.n_kv_heads + 1, shape.head_dim)
+    x = torch.zeros(batch.total_tokens, shape.d_model, device="cuda")
+    for cache in (fewer, other, heads):
+        for call in (lambda: A.arb_prefill(model, cache, db), lambda: A.arb_score_steps(model, cache, db, 0.0),
+                     lambda: A.arb_stage_layers(model, cache, db, 0, 1, x)):
+            with pytest.raises(ValueError):
+                call()
+    with pytest.raises(ValueError):
+        A.KVCache8.empty(1, 2, 2, 64, device="cpu")
+
+
 def test_two_calls_at_once_on_two_streams(A):
     heads = "router"
     hq, hkv, hd = HEADS[heads]
