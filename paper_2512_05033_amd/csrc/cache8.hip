@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v) {
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  for (int o = 1; o < LANES; o *= 2) v += __shfl_xor(v, o, 64);
   return v;
 }
 
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
     if (g) {
       float f = 1.0f;
       auto mean_square = [&] {                             // of f x
-        float sum[PAIRS / 4];                              // of every four pairs by itself, joined last: the same order for both widths
+        float sum[PAIRS / 4];                              // of every four pairs by itself, neighbours joined first: the same order for both widths
 #pragma unroll
         for (int w = 0; w < PAIRS / 4; ++w) {
           sum[w] = 0.f;
@@ -203,9 +203,8 @@ __global__ __launch_bounds__(256) void norm_rope_append_kernel(AppendArgs a) {
           for (int e = 0; e < 4; ++e) sum[w] += (f * x[4 * w + e]) * (f * x[4 * w + e]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[w] += (f * x[PAIRS + 4 * w + e]) * (f * x[PAIRS + 4 * w + e]);
-          sum[w] = row_sum<LANES>(sum[w]);
         }
-        return (PAIRS == 8 ? sum[0] + sum[PAIRS / 4 - 1] : sum[0]) * (1.0f / HD);
+        return row_sum<LANES>(PAIRS == 8 ? sum[0] + sum[PAIRS / 4 - 1] : sum[0]) * (1.0f / HD);
       };
       float mean = mean_square();
       if (mean == INFINITY) {                              // squares beyond fp32: those of 2^-64 x, and eps is nothing beside them
