@@ -240,7 +240,8 @@ extern "C" size_t arb_workspace_bytes(const arb_model *m, int32_t max_batch, int
   const long long few_tokens = (long long)max_batch * (kFewRows / G);
   const int few = few_tokens < max_total_tokens ? (int)few_tokens : max_total_tokens;
   const size_t few_bytes = attention_few_ws_bytes(attention_few_parts_cap(max_ctx), few, m->cfg.n_q_heads, m->cfg.head_dim);
-  return carve(m->cfg, max_total_tokens, splits, items, nullptr, few_bytes).total;
+  const size_t fine_bytes = attention_fine_ws_bytes(max_total_tokens, max_ctx, m->cfg.n_q_heads, G, m->cfg.head_dim);
+  return carve(m->cfg, max_total_tokens, splits, items, nullptr, few_bytes > fine_bytes ? few_bytes : fine_bytes).total;
 }
 
 // --------------------------------------------------------------- batch validation
@@ -337,8 +338,10 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
   FewPlan few_plan{};
   if (few_rows) few_plan = plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows, kv.kv8);
   const size_t few_bytes = few_rows ? attention_few_ws_bytes(few_plan.parts, T, c.n_q_heads, c.head_dim) : 0;
+  // (the static scratch does not grow with the batch, so no call asks it for more parts than it must)
+  const bool fine = (kv.kv8 || m->softcap > 0.f) && !ws_is_static;
   AttnPlan plan = few_rows ? AttnPlan{ATTN_KT, 1, 1, 0}    // (no splits of the other kernel)
-                           : plan_attention(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
+                           : (fine ? plan_attention_fine : plan_attention)(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   // the attention part is sized by this call's own split count (never above what arb_workspace_bytes assumed)
   Workspace w = carve(c, T, plan.max_splits, plan.n_items, ws, few_bytes);
   // Scratch that has no room for the attention work list (the static buffer's size does not follow from the batch) is used
@@ -784,7 +787,8 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
                                 max_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out, ws, ws_bytes, batch->prefix_lens,
                                 batch->cu_step_lens, (hipStream_t)stream, q_scaled != 0);
   }
-  AttnPlan plan = plan_attention(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
+  const bool fine = cache.k_scale || cache.softcap > 0.f;
+  AttnPlan plan = (fine ? plan_attention_fine : plan_attention)(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   hipStream_t st = (hipStream_t)stream;
   // Writing the work list costs a single call 2 to 8 us (a forward writes it once for all layers), and it pays where it leaves out
   // many empty places: 64 contexts of 100 to 6400 keys with steps of 16 to 79 tokens (2.7 and 2.2 places per item) 46 us with

@@ -518,6 +518,8 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(const bf16 *__rest
 static const int kTargetWorkgroups = 512;    // two resident workgroups per CU on 256 CUs
 static const int kMinChunk = 256, kMaxChunk = 4096, kMaxChunkDecode = 6144, kMaxSplits = 64;
 static const double kReplanUs = 20;
+static const int kFineSplits = 32;
+static const long long kFineRows = 65536;    // most rows of partial results in a plan of finer parts: 128 each for twice the CUs
 static const int kMaxRun = 16;                // longest run of work items on one XCD when there are few runs per XCD
 
 float attention_q_scale(int head_dim) { return (float)(1.4426950408889634 / sqrt((double)head_dim)); }
@@ -567,6 +569,21 @@ static double plan_us(int batch, const int32_t *prefix_host, const int32_t *cu_h
   return splits > 1 ? us + 5.0 + 1.3 * ceil_div(splits, 8) + parts * head_dim * 4e-7 : us;
 }
 
+static AttnPlan plan_of_chunk(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int chunk,
+                              int max_ctx, int max_step) {
+  AttnPlan pl;
+  pl.max_qtiles = ceil_div(max_step * G, QROWS);
+  pl.kv_chunk = chunk;
+  pl.max_splits = max_ctx > 0 ? ceil_div(max_ctx, pl.kv_chunk) : 1;
+  pl.n_items = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s, c = attn_seq_chunk(ctx, pl.kv_chunk);
+    for (int begin = 0; begin < ctx; begin += c)
+      pl.n_items += (ceil_div(s * G, QROWS) - attn_first_qtile(prefix_host[b], G, begin)) * n_kv_heads;
+  }
+  return pl;
+}
+
 AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim) {
   long long keys_streamed = 0;          // sum over (sequence, kv head, query tile) of the context length
   int max_ctx = 0, max_step = 0;
@@ -609,17 +626,33 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
     }
     chunk = pick;
   }
-  AttnPlan pl;
-  pl.max_qtiles = ceil_div(max_step * G, QROWS);
-  pl.kv_chunk = (int)chunk;
-  pl.max_splits = max_ctx > 0 ? ceil_div(max_ctx, pl.kv_chunk) : 1;
-  pl.n_items = 0;
+  return plan_of_chunk(batch, prefix_host, cu_host, G, n_kv_heads, (int)chunk, max_ctx, max_step);
+}
+
+// Few workgroups, contexts of more than kMinChunk keys: the launch is the latency of one part, and a tile (1.4 us) costs more than
+// another part does in the merge.  Parts of 64 keys where eight of them do (one round of the merge), otherwise of 128 or more, at most
+// kFineSplits, and no more workgroups than there are CUs: two of them on a CU would share its pipes, and the merge grows.
+// (e4m3, us of a call, parts of 256 keys -> these: 8B shape, 41 tokens on 360 15.1 -> 11.2, 16 on 1000 14.8 -> 11.9, 64 on 4000 20.4
+// (128 keys: 23.6); 1.5B shape, 64 on 2000 16.4 -> 15.0 (64 keys: 17.4), 20 on 700 15.1 -> 12.0, 4 x 7 on 279 to 654 14.3 -> 11.3, 30 on 8000 20.1 (128
+// keys in 63 parts: 22.7).)
+// The uncapped launch over bf16 pools keeps the parts, and with them the results, that it has always had.
+AttnPlan plan_attention_fine(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim) {
+  long long keys_streamed = 0;
+  int max_ctx = 0, max_step = 0;
   for (int b = 0; b < batch; ++b) {
-    const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s, c = attn_seq_chunk(ctx, pl.kv_chunk);
-    for (int begin = 0; begin < ctx; begin += c)
-      pl.n_items += (ceil_div(s * G, QROWS) - attn_first_qtile(prefix_host[b], G, begin)) * n_kv_heads;
+    const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s;
+    keys_streamed += (long long)ceil_div(s * G, QROWS) * n_kv_heads * ctx;
+    max_ctx = ctx > max_ctx ? ctx : max_ctx;
+    max_step = s > max_step ? s : max_step;
   }
-  return pl;
+  const long long cus = kTargetWorkgroups / 2, least = max_ctx <= 8 * KT ? KT : 2 * KT;
+  long long chunk = (keys_streamed / cus + KT - 1) / KT * KT;
+  if (chunk < least) chunk = least;
+  while (max_ctx > chunk * kFineSplits) chunk += KT;
+  if (max_ctx <= kMinChunk || chunk >= kMinChunk ||
+      (long long)cu_host[batch] * G * n_kv_heads * ceil_div(max_ctx, (int)chunk) > kFineRows)
+    return plan_attention(batch, prefix_host, cu_host, G, n_kv_heads, head_dim);
+  return plan_of_chunk(batch, prefix_host, cu_host, G, n_kv_heads, (int)chunk, max_ctx, max_step);
 }
 
 // Workspace: partial results [splits, T, Hq, hd] bf16 and their (m, l) fp32 (none with a single split), the splits of every
@@ -634,6 +667,16 @@ static size_t part_ml_bytes(int max_splits, int T, int Hq) {
 size_t attention_ws_bytes(int max_splits, size_t n_items, int total_tokens, int n_q_heads, int head_dim) {
   return part_acc_bytes(max_splits, total_tokens, n_q_heads, head_dim) + part_ml_bytes(max_splits, total_tokens, n_q_heads) +
          align_up((size_t)total_tokens * sizeof(int32_t), 256) + align_up(n_items * sizeof(AttnItem), 256);
+}
+
+size_t attention_fine_ws_bytes(int total_tokens, int max_ctx, int n_q_heads, int G, int head_dim) {
+  if (max_ctx <= kMinChunk) return 0;
+  const int splits = ceil_div(max_ctx, KT) < kFineSplits ? ceil_div(max_ctx, KT) : kFineSplits;
+  long long rows = (long long)total_tokens * n_q_heads * splits;
+  if (rows > kFineRows) rows = kFineRows;
+  const size_t tokens = total_tokens < kFineRows ? total_tokens : kFineRows;
+  // (an item is at least one token's rows against one part)
+  return rows * (head_dim * sizeof(bf16) + 2 * sizeof(float)) + tokens * sizeof(int32_t) + rows / G * sizeof(AttnItem) + 4 * 256;
 }
 
 AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int n_q_heads, int head_dim) {

@@ -146,6 +146,9 @@ static __host__ __device__ inline int attn_first_qtile(int prefix, int G, int kv
   return kv_begin <= prefix ? 0 : (int)((long long)(kv_begin - prefix) * G / ATTN_QROWS);
 }
 AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim);
+// The same for the launches over an 8-bit cache or with capped scores, and the most workspace that its own choices need.
+AttnPlan plan_attention_fine(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim);
+size_t attention_fine_ws_bytes(int total_tokens, int max_ctx, int n_q_heads, int G, int head_dim);
 size_t attention_ws_bytes(int max_splits, size_t n_items, int total_tokens, int n_q_heads, int head_dim);
 int attention_splits_cap(int max_ctx);   // largest max_splits plan_attention can return for contexts <= max_ctx
 // The work list inside an attention workspace (attention_ws_bytes), to be written by launch_token_meta before the

@@ -121,3 +121,11 @@ def few_plan(lib, n_kv_heads, head_dim, prefix, steps, max_rows, kv8=True) -> Fe
     f.restype, f.argtypes = FewPlan, [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_bool]
     p, cu = np.asarray(prefix, np.int32), np.concatenate([[0], np.cumsum(steps)]).astype(np.int32)
     return f(len(p), p.ctypes.data, cu.ctypes.data, n_kv_heads, head_dim, max_rows, kv8)
+
+
+def fine_attention_plan(lib, m: W.ModelShape, prefix, steps) -> AttentionPlan:
+    """The plan over an 8-bit cache or with capped scores (a host function that the header does not declare)."""
+    f = lib._Z19plan_attention_fineiPKiS0_iii
+    f.restype, f.argtypes = AttentionPlan, [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int]
+    p, cu = np.asarray(prefix, np.int32), np.concatenate([[0], np.cumsum(steps)]).astype(np.int32)
+    return f(len(p), p.ctypes.data, cu.ctypes.data, m.group, m.n_kv_heads, m.head_dim)

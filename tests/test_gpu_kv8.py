@@ -315,9 +315,14 @@ CASES = [
 ]
 
 
+# what the long-step kernel cuts into parts of 64, 128 and 192 keys
+FINE = [("target", [360], [41]), ("router", [449, 3], [60, 7]), ("router", [2000], [64]), ("tiny", [50], [1200]), ("multi", [92, 5623], [9, 11]),
+        ("single", [11], [570]), ("target", [74, 302, 0], [39, 126, 257]), ("multi", [0], [257])]
+
+
 @pytest.mark.parametrize("kv8", [True, False])
 @pytest.mark.parametrize("cap,q_scaled", [(0.0, True), (0.0, False), (20.0, True), (5.0, False)])
-@pytest.mark.parametrize("heads,prefix,steps", CASES)
+@pytest.mark.parametrize("heads,prefix,steps", CASES + FINE)
 def test_attention(A, heads, prefix, steps, cap, q_scaled, kv8):
     hq, hkv, hd = HEADS[heads]
     db, tables, n = make_batch(A, prefix, steps, 21)
@@ -370,8 +375,10 @@ def test_attention_with_scores_that_jump(A, heads, prefix, steps, cap):
     assert bool(((got.double().view(ref.shape) - ref).abs() <= (4.3 * U + 4 * 2.0 ** -10) * mag + 1e-30).all())
 
 
-@pytest.mark.parametrize("heads,prefix,steps", [("router", [300, 77, 1000], [50, 64, 33]), ("tiny", [100, 4500], [4100, 20])])
-@pytest.mark.parametrize("cap", [0.0, 30.0])
+# (without a cap the two are cut into the same parts from 256 workgroups on, see the plan of finer parts)
+@pytest.mark.parametrize("heads,prefix,steps,cap", [
+    ("router", [300, 77, 1000], [50, 64, 33], 30.0), ("router", [3000, 770, 10500], [50, 64, 33], 0.0),
+    ("tiny", [100, 4500], [4100, 20], 0.0), ("tiny", [100, 4500], [4100, 20], 30.0)])
 def test_long_steps_are_the_attention_over_the_unpacked_cache_bit_for_bit(A, heads, prefix, steps, cap):
     """What an element and its scale stand for is exact in bf16, so where one kernel serves both caches the products are the same."""
     hq, hkv, hd = HEADS[heads]
@@ -582,7 +589,7 @@ def test_two_calls_at_once_on_two_streams(A):
 
 
 @pytest.mark.parametrize("heads,prefix,steps", [("router", [130 * i % 7001 for i in range(70)], [1] * 70), ("target", [4000, 20, 9000], [2, 8, 1]),
-                                                ("router", [3000, 300], [40, 64])])
+                                                ("router", [3000, 300], [40, 64]), ("target", [360], [41])])
 def test_nothing_is_written_outside_of_the_least_workspace(A, heads, prefix, steps):
     import re
     hq, hkv, hd = HEADS[heads]

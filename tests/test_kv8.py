@@ -211,6 +211,31 @@ def test_every_tile_of_a_decoding_batch_has_a_place(lib):
     assert len(seen) == 3                                        # in a row, even, uncut
 
 
+def test_parts_of_few_workgroups_are_fine_ones(lib):
+    """Random batches: finer parts than 256 keys only where those would leave CUs empty, at most 32 of them and 65536 rows of partial
+    results; otherwise the plan of the uncapped bf16 launch."""
+    from helpers import attention_plan, fine_attention_plan
+    import workloads as W
+    rng = np.random.default_rng(2)
+    finer = 0
+    for _ in range(600):
+        m = [W.TINY, W.ROUTER_1P5B, W.TARGET_8B][rng.integers(3)]
+        batch, hi = int(np.exp(rng.uniform(0, np.log(40)))), int(np.exp(rng.uniform(0, np.log(40000))))
+        prefix, steps = rng.integers(0, hi + 1, batch), rng.integers(1, int(rng.choice([12, 80, 600])), batch)
+        fine, plain = fine_attention_plan(lib, m, prefix, steps), attention_plan(lib, m, prefix, steps)
+        longest = int((prefix + steps).max())
+        if fine.kv_chunk >= 256:
+            assert all(getattr(fine, f) == getattr(plain, f) for f, _ in fine._fields_)
+            continue
+        finer += 1
+        assert fine.kv_chunk % 64 == 0 and fine.kv_chunk >= (64 if longest <= 512 else 128) and longest > 256
+        assert fine.max_splits == -(-longest // fine.kv_chunk) <= 32
+        assert int(steps.sum()) * m.n_q_heads * fine.max_splits <= 65536
+        streamed = sum(-(-int(s) * m.group // 128) * m.n_kv_heads * int(p + s) for p, s in zip(prefix, steps))
+        assert streamed < 256 * 256
+    assert finer > 50
+
+
 def test_workspace_covers_a_decoding_batch(lib):
     """arb_workspace_bytes is enough for what a call on an 8-bit cache asks for (a refusal names it)."""
     import re
@@ -222,7 +247,7 @@ def test_workspace_covers_a_decoding_batch(lib):
     rng = np.random.default_rng(1)
     for _ in range(300):
         batch, hi = int(np.exp(rng.uniform(0, np.log(100)))), int(np.exp(rng.uniform(0, np.log(100000))))
-        prefix, steps = rng.integers(0, hi + 1, batch), rng.integers(1, int(rng.choice([2, 17, 80])), batch)
+        prefix, steps = rng.integers(0, hi + 1, batch), rng.integers(1, int(rng.choice([2, 17, 80, 500])), batch)
         bt = _batch(B, prefix, np.concatenate([[0], np.cumsum(steps)]), 1 << 14)
         assert lib.arb_score_steps_kv8(h, C.byref(kv), C.byref(bt), 0.0, P, None, None, P, 16, None) == B.ARB_ECAPACITY
         need = int(re.search(rb"workspace 16 < (\d+) bytes", lib.arb_last_error()).group(1))
