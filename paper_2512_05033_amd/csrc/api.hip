@@ -498,7 +498,7 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
                                  c.head_dim, few_plan, w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
       else
         s = launch_attention(w.q, hq, cache, bt->block_tables, bt->max_blocks_per_seq, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan,
-                             w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true);
+                             w.attn, w.attn_ws, w.attn_ws_bytes, bt->prefix_lens, bt->cu_step_lens, st, true, max_rows);
     }
     if (s) return s;
     {
@@ -806,7 +806,7 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
       return s;
   return launch_attention((const bf16 *)q, q_row_stride, cache, batch->block_tables,
                           batch->max_blocks_per_seq, batch->batch, T, c.n_q_heads, c.n_kv_heads, c.head_dim, plan, (bf16 *)out,
-                          ws, ws_bytes, batch->prefix_lens, batch->cu_step_lens, st, q_scaled != 0, plan.n_items == 0);
+                          ws, ws_bytes, batch->prefix_lens, batch->cu_step_lens, st, q_scaled != 0, max_rows, plan.n_items == 0);
 }
 
 extern "C" arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,

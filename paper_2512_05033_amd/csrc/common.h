@@ -168,7 +168,7 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
                             const int32_t *block_tables, int max_blocks_per_seq, int batch, int total_tokens, int n_q_heads,
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
                             const int32_t *prefix_lens, const int32_t *cu_step_lens, hipStream_t st, bool q_prescaled,
-                            bool count_splits = false);   // count_splits: no launch_token_meta has written the tokens' splits
+                            int max_rows, bool count_splits = false);   // max_rows: of a sequence and kv head; count_splits: no launch_token_meta has written the tokens' splits
 // attention_few.hip: few query rows (step tokens x query heads of one kv head) over an 8-bit cache, or capped.
 struct FewPlan {
   int per;                 // 64-key tiles of a workgroup, at most
