@@ -338,8 +338,7 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
   FewPlan few_plan{};
   if (few_rows) few_plan = plan_attention_few(B, bt->prefix_lens_host, bt->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows, kv.kv8);
   const size_t few_bytes = few_rows ? attention_few_ws_bytes(few_plan.parts, T, c.n_q_heads, c.head_dim) : 0;
-  // (the static scratch does not grow with the batch, so no call asks it for more parts than it must)
-  const bool fine = (kv.kv8 || m->softcap > 0.f) && !ws_is_static;
+  const bool fine = kv.kv8 || m->softcap > 0.f;
   AttnPlan plan = few_rows ? AttnPlan{ATTN_KT, 1, 1, 0}    // (no splits of the other kernel)
                            : (fine ? plan_attention_fine : plan_attention)(B, bt->prefix_lens_host, bt->cu_step_lens_host, G, c.n_kv_heads, c.head_dim);
   // the attention part is sized by this call's own split count (never above what arb_workspace_bytes assumed)

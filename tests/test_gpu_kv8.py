@@ -750,6 +750,19 @@ def test_prompts_enter_the_cache_and_steps_are_scored_against_them(A, name, step
     assert rel_err(x.double().cpu().numpy(), whole.double().cpu().numpy()) < 1e-2
 
 
+@pytest.mark.parametrize("steps", [2, 7, 40])
+def test_capped_scores_without_allocation_are_those_with_a_workspace(A, steps):
+    w = W.Workload("kv8", W.TINY, 3, (100, 900), ("fixed", steps, steps), "shuffled", "prefill", 0.0, ("const", 0.0), 780)
+    batch, weights, gains, model, kv, db = _forward_session(A, w, 6, 20.0, True, kv8=False)
+    A.arb_prefill(model, kv, H().prompt_batch(w, batch))
+    want, esc, _ = A.arb_score_steps(model, kv, db, 0.0)
+    got, also = torch.empty_like(want), torch.empty_like(esc)
+    for _ in range(2):
+        got.fill_(float("nan"))
+        A.arb_score_steps_noalloc(model, kv, db, 0.0, scores=got, escalate=also)
+        assert bool(torch.isfinite(want).all()) and torch.equal(got, want) and torch.equal(also, esc)
+
+
 def test_a_captured_pass_on_the_8bit_cache_replays(A):
     w = W.Workload("kv8", W.TINY, 3, (100, 900), ("uniform", 1, 4), "shuffled", "prefill", 0.0, ("const", 0.0), 778)
     batch, weights, gains, model, kv, db = _forward_session(A, w, 4, 30.0, True)
