@@ -24,8 +24,8 @@
 //
 // An 8-bit cache (e4m3 elements, a power-of-two scale per row) goes through registers: a thread loads 16 elements of a
 // row and the row's scale, v_cvt_scalef32_pk_bf16_fp8 makes two bf16 of two elements and the scale, exactly, and the
-// stages in LDS are those of the bf16 cache.  So a tile is converted once per workgroup, not once per wave, and the rest
-// is the same kernel: the products are, bit for bit, those over the cache's bf16 values.
+// stages in LDS are those of the bf16 cache.  So a tile is converted once per workgroup, not once per wave, and the products are,
+// bit for bit, those over the cache's bf16 values.
 #include "attention_merge.h"
 #include "common.h"
 
@@ -37,6 +37,7 @@ constexpr int QROWS = ATTN_QROWS, KT = ATTN_KT;
 constexpr float kLazyLog2 = 8.0f;   // growth of a row maximum (log2 units) that forces a rescale
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 #define GLOBAL_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
 #define LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
@@ -77,8 +78,10 @@ __device__ __forceinline__ int v_off(int key, int chunk) { return key * HD + ((c
 // matrix pipe cannot start from the reference; but it is linear in r, so the maximum is a minimum of r, and cap and
 // reference are one FMA in front of the exponential.  scale_log2 is then cap_in.
 //
-// NT: 32-key halves of the tile that the wave takes, from sk, sv and ts on.
-template <int HD, bool PRESCALED, bool CAP, int NT>
+// NT: 32-key halves of the tile that the wave takes, from sk, sv and ts on.  HEAD: log2 of the room that the reference leaves above the
+// maximum: weights may grow to 2^kLazyLog2 of it and sum up over the keys, and the accumulators are to hold values near the largest of
+// bf16 all the same (0 for the uncapped bf16 form, whose results stay as they were).
+template <int HD, bool PRESCALED, bool CAP, int NT, int HEAD>
 __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, const bf16x8 (&qf)[HD / 16], f32x16 (&o)[HD / 32],
                                             f32x16 &negm, float &m_run, float &l_run, int ts, int limit, float scale_log2,
                                             float cap_out, int col, int half, int lane) {
@@ -139,14 +142,14 @@ __device__ __forceinline__ void attend_tile(const bf16 *sk, const bf16 *sv, cons
   if (CAP) mx = fmaf(-2.f * cap_out, mx, cap_out + negm[0]);
   else if (!PRESCALED) mx = fmaf(mx, scale_log2, negm[0]);
   // The reference maximum m_run is advanced only when some row's maximum has outgrown it by more
-  // than kLazyLog2: until then exp2(s - m_run) <= 2^kLazyLog2, far inside the range of bf16 and
+  // than kLazyLog2 (m_run is that maximum plus HEAD): until then exp2(s - m_run) <= 2^(kLazyLog2 - HEAD), inside the range of bf16 and
   // fp32, and o / l is unchanged because both carry the same factor.  Most tiles then skip the
   // rescaling of the accumulators.  A row without a visible key so far has m_run = -inf and the
   // reference 0; its first visible key always sets the reference.
-  if (__builtin_amdgcn_ballot_w64(mx > kLazyLog2 || (m_run == -INFINITY && mx > -INFINITY)) != 0) {
+  if (__builtin_amdgcn_ballot_w64(mx > kLazyLog2 - HEAD || (m_run == -INFINITY && mx > -INFINITY)) != 0) {
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
-    const float m_new = fmaxf(m_run, m_use + mx);                    // -inf only while nothing is visible
+    const float m_new = fmaxf(m_run, m_use + (mx + HEAD));           // -inf only while nothing is visible
     const float m_new_use = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new_use);   // m_run = -inf -> 0
     l_run *= alpha;
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   auto attend = [&](const bf16 *sk, const bf16 *sv, int t) {
     const int key0 = PAIRED ? (wave_u >> 1) * 32 : 0;      // (a multiple of 32 keys changes no swizzle)
     if (wave_active)
-      attend_tile<HD, PRESCALED, CAP, PAIRED ? 1 : 2>(sk + key0 * HD, sv + key0 * HD, qf, o, negm, m_run, l_run, kv_begin + t * KT + key0, limit,
+      attend_tile<HD, PRESCALED, CAP, PAIRED ? 1 : 2, KV8 || CAP ? ATTN_HEADROOM : 0>(sk + key0 * HD, sv + key0 * HD, qf, o, negm, m_run, l_run, kv_begin + t * KT + key0, limit,
                                                       scale_log2, cap_out, col, half, lane);
   };
   const int last_tile = n_tiles - 1;
@@ -482,17 +485,39 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
   const size_t orow = (size_t)(tok0 + tok_i) * Hq + head;   // (token, head) index
   if (!wave_active) return;
-  // With SPLIT this is the split's own normalised result in bf16 (it lies in the hull of the values, like the output)
-  // plus its (m, l) in fp32: half the partial traffic of fp32 accumulators.
+  // With SPLIT this is the split's own normalised result (it lies in the hull of the values, like the output) in 16 bits plus its
+  // (m, l) in fp32: half the partial traffic of fp32 accumulators.  bf16 over an uncapped bf16 cache, as ever; otherwise fp16
+  // relative to a power of two that puts the row's largest at 2^14, with three bits more (error against 64 bits, 16 steps of 64 in five
+  // parts: 0.0023 of the result's norm in bf16, 0.0017 this way, 0.0016 with one rounding, the result's).
+  constexpr bool RELATIVE = SPLIT && (KV8 || CAP);
   const float inv = !SPLIT || l_tot > 0.f ? 1.0f / l_tot : 0.f;
+  float scale = 1.f, rel = 1.f;
+  if constexpr (RELATIVE) {
+    float most = 0.f;                                       // of the finite ones: an infinity stays one in fp16
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = fabsf(o[mt][r]);
+        most = fmaxf(most, x < INFINITY ? x : 0.f);
+      }
+    most = fmaxf(most, __shfl_xor(most, 32, 64)) * inv;
+    const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 27), 254);       // exponent + 127, from 2^-100 on
+    scale = __builtin_bit_cast(float, (e - 14) << 23);
+    rel = __builtin_bit_cast(float, (254 - (e - 14)) << 23);
+  }
   constexpr int CPR = HD / 8, RPS = 64 / CPR;               // 16-byte chunks per row, rows per store
   bf16 *dst = SPLIT ? part_acc + (size_t)split * T * Hq * HD : out;
   const int rows_here = min(32, rows - row0 - row_wave * 32);
   auto piece = [&](int mt, int r4) {
     bf16x4 v;
+    f16x4 h;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[mt][r4 * 4 + e] * inv);
-    return v;
+    for (int e = 0; e < 4; ++e) {
+      v[e] = (bf16)(o[mt][r4 * 4 + e] * inv);
+      h[e] = (_Float16)(o[mt][r4 * 4 + e] * inv * rel);
+    }
+    return RELATIVE ? __builtin_bit_cast(bf16x4, h) : v;
   };
   if (__builtin_amdgcn_readfirstlane(rows_here) < 16) {
     if (row_ok) {
@@ -518,8 +543,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   }
   if (SPLIT && half == 0 && row_ok) {
     float *ml = part_ml + ((size_t)split * T * Hq + orow) * 2;
-    ml[0] = m_run;
-    ml[1] = l_tot;
+    ml[0] = RELATIVE ? m_run + __builtin_amdgcn_logf(l_tot) : m_run;   // (v_log_f32: base 2)
+    ml[1] = RELATIVE ? scale : l_tot;
     // the number of splits that the merge reads for a token, where no earlier launch has written it
     if (tok_splits && split == 0 && hk == 0) tok_splits[tok0 + tok_i] = min(limit / attn_seq_chunk(ctx, kv_chunk) + 1, max_splits);
   }
@@ -527,8 +552,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
 
 // Merge of the split partials.  A thread owns eight consecutive elements of one (token, head) row, so a workgroup of 256 merges
 // 2048 / HD rows.
-template <int HD>
-__global__ __launch_bounds__(256) void attention_merge_kernel(const bf16 *__restrict__ part_acc,
+template <int HD, typename Part>
+__global__ __launch_bounds__(256) void attention_merge_kernel(const Part *__restrict__ part_acc,
                                                               const float *__restrict__ part_ml,
                                                               const int32_t *__restrict__ tok_splits, int max_splits, int T,
                                                               int Hq, bf16 *__restrict__ out) {
@@ -762,12 +787,12 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   ARB_CHECK_LAUNCH("attention");
   if (split) {
     const dim3 mgrid(ceil_div(total_tokens * n_q_heads, 2048 / head_dim)), mblock(256);
-    if (head_dim == 128)
-      hipLaunchKernelGGL((attention_merge_kernel<128>), mgrid, mblock, 0, st, part_acc, part_ml, lists.tok_splits, plan.max_splits,
-                         total_tokens, n_q_heads, out);
-    else
-      hipLaunchKernelGGL((attention_merge_kernel<64>), mgrid, mblock, 0, st, part_acc, part_ml, lists.tok_splits, plan.max_splits,
-                         total_tokens, n_q_heads, out);
+#define ARB_ATTN_MERGE(HD, Part)                                                                                   \
+  hipLaunchKernelGGL((attention_merge_kernel<HD, Part>), mgrid, mblock, 0, st, (const Part *)part_acc, part_ml, lists.tok_splits, \
+                     plan.max_splits, total_tokens, n_q_heads, out)
+    if (kv8 || capped) { if (head_dim == 128) ARB_ATTN_MERGE(128, _Float16); else ARB_ATTN_MERGE(64, _Float16); }
+    else               { if (head_dim == 128) ARB_ATTN_MERGE(128, bf16); else ARB_ATTN_MERGE(64, bf16); }
+#undef ARB_ATTN_MERGE
     ARB_CHECK_LAUNCH("attention_merge");
   }
   return ARB_OK;

@@ -274,10 +274,11 @@ __global__ __launch_bounds__(256, HD == 64 && NQ == 1 && KV8 ? 4 : 2) void atten
             st[t][n][e] = x;
             mx[n] = fmaxf(mx[n], x);
           }
+        mx[n] += ATTN_HEADROOM;
         grows |= mx[n] > m_run[n] + kLazyLog2;               // m_run = -inf: any visible key
       }
-      // The reference maximum moves only when a row has outgrown it by 2^8 (until then every weight is at most 2^8,
-      // and the quotient is the same); the four lanes of a query share it, and so do its accumulators.
+      // The reference moves only when a row has outgrown it by 2^8, and is set 2^16 above the row's maximum (so every weight is at most
+      // 2^-8 and sums of values near the largest of bf16 stay in fp32; the quotient is the same); the four lanes of a query share it, and so do its accumulators.
       if (__builtin_amdgcn_ballot_w64(grows) != 0) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {

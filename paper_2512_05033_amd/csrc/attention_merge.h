@@ -6,7 +6,8 @@
 #include <math.h>
 
 // Of one (token, head) row: sum_s w_s l_s o_s and sum_s w_s l_s with w_s = exp2(m_s - m), m = max_s m_s and o_s the split's
-// normalised result.  A thread owns eight consecutive elements (`piece`) of the row; idx = token * Hq + head, stride = T * Hq.
+// normalised result.  Beside a result in fp16 stand m_s + log2(l_s), which is all that the weight needs, and the power of two that it is
+// relative to.  A thread owns eight consecutive elements (`piece`) of the row; idx = token * Hq + head, stride = T * Hq.
 struct SplitSum {
   float m, l, acc[8];
   __device__ __forceinline__ void clear() {
@@ -18,11 +19,12 @@ struct SplitSum {
   // Splits first, first + step, ... below n_splits, eight at a time: all their loads go out together (a loop over a run-time count
   // waits for each before it asks for the next), then they are combined under their common maximum; groups of eight are
   // chained by the usual online rescaling.
-  // Part: bf16 or float.
+  // Part: bf16, _Float16 or float.
   template <int HD, typename Part>
   __device__ __forceinline__ void add(const Part *__restrict__ part_acc, const float *__restrict__ part_ml, size_t stride,
                                       size_t idx, int piece, int first, int step, int n_splits) {
     typedef Part part8 __attribute__((ext_vector_type(8)));
+    constexpr bool RELATIVE = __is_same(Part, _Float16);
     for (int s0 = first; s0 < n_splits; s0 += 8 * step) {
       float2 ml[8];
       part8 v[8];
@@ -49,10 +51,10 @@ struct SplitSum {
       for (int e = 0; e < 8; ++e) acc[e] *= keep;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float w = exp2f(ml[j].x - ref) * ml[j].y;  // a split without visible keys: exp2(-inf) * 0 = 0
+        const float x = exp2f(ml[j].x - ref), w = RELATIVE ? x : x * ml[j].y, f = x * ml[j].y;   // a split without visible keys: exp2(-inf) * 0 = 0
         l += w;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += w * (float)v[j][e];
+        for (int e = 0; e < 8; ++e) acc[e] += f * (float)v[j][e];
       }
     }
   }

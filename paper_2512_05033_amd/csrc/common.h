@@ -123,6 +123,7 @@ arb_status launch_gemm_few_gate_up(const bf16 *x, const bf16 *B, bf16 *act, int 
 // attention.hip
 constexpr int ATTN_QROWS = 128;     // query rows (step tokens x query heads of one kv head) per workgroup
 constexpr int ATTN_KT = 64;         // keys per tile
+constexpr int ATTN_HEADROOM = 16;   // log2 of how far the softmax's reference is set above the maximum (8-bit and capped forms)
 struct AttnPlan {
   int kv_chunk;      // most keys per split (multiple of 64)
   int max_splits;    // ceil(max_ctx / kv_chunk) over the batch

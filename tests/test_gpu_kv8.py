@@ -315,6 +315,25 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [2000, 300], [64, 9]), ("target", [700], [16]), ("tiny", [1500], [60]), ("router", [3000], [2])])
+@pytest.mark.parametrize("kv8,size", [(True, 1.0), (True, 1e30), (True, 1e-24), (False, 1.0), (False, 1e36), (False, 1e-33)])
+def test_parts_hold_values_of_any_size(A, heads, prefix, steps, kv8, size):
+    """Cut contexts whose values are large, small, and of columns that differ by 2^20 (2^12 where e4m3 has to hold both)."""
+    hq, hkv, hd = HEADS[heads]
+    db, tables, n = make_batch(A, prefix, steps, 25)
+    k, v = rows((n, hkv, 16, hd), 26, 0.8), rows((n, hkv, 16, hd), 27, 0.8).float() * size
+    v[..., ::7] *= 2.0 ** -12 if kv8 else 2.0 ** -20
+    kv = A.KVLayer(k, v.bfloat16())
+    if kv8:
+        plain, kv = kv, layer8(A, n, hkv, hd)
+        A.arb_kv8_pack(plain, kv)
+    q = queries(sum(steps), heads, 28, True)
+    got = A.arb_stage_attention_kv(stage_model(heads), q, kv, db, softcap=20.0, q_scaled=True)
+    ref, mag = attention_ref(heads, q, kv, tables, prefix, steps, 20.0, True)
+    # (bf16 and fp32 below 2^-126 round to a multiple of 2^-133)
+    assert bool(((got.double().view(ref.shape) - ref).abs() <= 4.3 * U * mag + 2.0 ** -132).all())
+
+
 # what the long-step kernel cuts into parts of 64, 128 and 192 keys
 FINE = [("target", [360], [41]), ("router", [449, 3], [60, 7]), ("router", [2000], [64]), ("tiny", [50], [1200]), ("multi", [92, 5623], [9, 11]),
         ("single", [11], [570]), ("target", [74, 302, 0], [39, 126, 257]), ("multi", [0], [257])]
@@ -375,21 +394,26 @@ def test_attention_with_scores_that_jump(A, heads, prefix, steps, cap):
     assert bool(((got.double().view(ref.shape) - ref).abs() <= (4.3 * U + 4 * 2.0 ** -10) * mag + 1e-30).all())
 
 
-# (without a cap the two are cut into the same parts from 256 workgroups on, see the plan of finer parts)
-@pytest.mark.parametrize("heads,prefix,steps,cap", [
-    ("router", [300, 77, 1000], [50, 64, 33], 30.0), ("router", [3000, 770, 10500], [50, 64, 33], 0.0),
-    ("tiny", [100, 4500], [4100, 20], 0.0), ("tiny", [100, 4500], [4100, 20], 30.0)])
-def test_long_steps_are_the_attention_over_the_unpacked_cache_bit_for_bit(A, heads, prefix, steps, cap):
-    """What an element and its scale stand for is exact in bf16, so where one kernel serves both caches the products are the same."""
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [300, 77, 1000], [50, 64, 33]), ("tiny", [100, 4500], [4100, 20]), ("router", [100, 77, 0], [50, 64, 250]), ("target", [700], [16])])
+def test_long_steps_are_the_attention_over_the_unpacked_cache_bit_for_bit(A, heads, prefix, steps):
+    """What an element and its scale stand for is exact in bf16, so where one form serves both caches the products are the same."""
     hq, hkv, hd = HEADS[heads]
     db, tables, n = make_batch(A, prefix, steps, 51)
     kv, plain = filled(A, n, hkv, hd, 52), layer16(A, n, hkv, hd)
     A.arb_kv8_unpack(kv, plain)
     q = queries(sum(steps), heads, 53, True)
-    run = lambda layer: A.arb_stage_attention_kv(stage_model(heads), q, layer, db, softcap=cap, q_scaled=True)
+    run = lambda layer: A.arb_stage_attention_kv(stage_model(heads), q, layer, db, softcap=30.0, q_scaled=True)
     assert torch.equal(run(kv), run(plain))
-    if cap == 0:
-        assert torch.equal(run(plain), A.arb_stage_attention(stage_model(heads), q, plain.k_pool, plain.v_pool, db, q_scaled=True))
+
+
+@pytest.mark.parametrize("heads,prefix,steps", [("router", [300, 77, 1000], [50, 64, 33]), ("tiny", [100, 4500], [4100, 20]), ("target", [700, 5], [16, 1]), ("router", [1531], [1])])
+@pytest.mark.parametrize("q_scaled", [True, False])
+def test_uncapped_over_bf16_is_the_stage_it_generalises_bit_for_bit(A, heads, prefix, steps, q_scaled):
+    hq, hkv, hd = HEADS[heads]
+    db, tables, n = make_batch(A, prefix, steps, 54)
+    kv, q = filled(A, n, hkv, hd, 55, kv8=False), queries(sum(steps), heads, 56, q_scaled)
+    got = A.arb_stage_attention_kv(stage_model(heads), q, kv, db, q_scaled=q_scaled)
+    assert torch.equal(got, A.arb_stage_attention(stage_model(heads), q, kv.k_pool, kv.v_pool, db, q_scaled=q_scaled))
 
 
 @pytest.mark.parametrize("heads,prefix,steps", [("router", [13, 40, 64], [1, 2, 1]), ("target", [5], [60]), ("tiny", [63, 1], [3, 1]), ("router", [600], [1]), ("target", [70, 1], [11, 2])])
