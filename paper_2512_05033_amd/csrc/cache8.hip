@@ -321,8 +321,8 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint8_t *__restrict__
 
 // Few tokens: a workgroup per 256 lanes of units and four pairs a lane, so that a token is one round of loads.  Many: eight pairs a
 // lane (16-byte accesses of bf16 rows) and, in a call of its own, two tokens per workgroup, whose angles two waves find at once.
-// (32/8 heads into the 8-bit cache, few / many: 600 tokens 6.2 / 7.3 us, 900 9.1 / 8.4, 3001 17.7 / 14.2 (4.8 TB/s, the rate of
-// a large copy), 12000 61.8 / 56.2.  Of the 14.2 the angles are 0.5; with one token per workgroup 17.1, with four 14.6.)
+// (32/8 heads into the 8-bit cache, few / many: 600 tokens 6.2 / 7.3 us, 900 9.1 / 8.4, 3001 17.7 / 14.6 (4.6 TB/s, nearly that of
+// a large copy), 12000 61.8 / 56.2.  Of the 14.6 the angles are 0.5; with one token per workgroup 17.1, with four 14.6.)
 constexpr int kAppendManyTokens = 768;
 
 template <bool PARTS, bool TABLE>
