@@ -735,13 +735,14 @@ def _layers(A, kv):
 
 @pytest.mark.parametrize("name,steps,norms,softcap,kv8", [
     ("tiny", 32, True, 30.0, True), ("tiny 4-bit", 33, True, 0.0, True), ("tiny 4-bit", 2, False, 20.0, True), ("tiny", 1, True, 0.0, True), ("tiny", 3, False, 0.0, True), ("router", 5, True, 20.0, True),
-    ("tiny long", 2, True, 0.0, True), ("tiny long", 3, True, 15.0, False), ("router", 1, False, 30.0, True), ("tiny", 2, True, 10.0, False), ("tiny", 40, False, 25.0, False)])
+    ("tiny long", 2, True, 0.0, True), ("tiny long", 3, True, 15.0, False),
+    ("tiny long", 40, True, 0.0, True), ("tiny long", 33, False, 25.0, False), ("tiny 4-bit long", 20, False, 30.0, True), ("router", 1, False, 30.0, True), ("tiny", 2, True, 10.0, False), ("tiny", 40, False, 25.0, False)])
 def test_prompts_enter_the_cache_and_steps_are_scored_against_them(A, name, steps, norms, softcap, kv8):
     """arb_prefill of whole prompts, then arb_score_steps of a drafted step on the same cache: the cache is what the oracle stores
     up to its rounding, and the hidden states and scores are the oracle's over that cache."""
     from helpers import HIDDEN_TOL, SCORE_TOL, rel_err
     from dataclasses import replace
-    four_bit = name.endswith("4-bit")
+    four_bit = "4-bit" in name
     shape = W.TINY if name.startswith("tiny") else replace(W.ROUTER_1P5B, n_layers=2, vocab=4096)
     w = W.Workload("kv8", shape, 3, (300, 600) if name.endswith("long") else (40, 230), ("fixed", steps, steps), "shuffled", "prefill", 0.0, ("const", 0.0), 777)
     batch, weights, gains, model, kv, db = _forward_session(A, w, 3, softcap, norms, kv8, four_bit)
@@ -787,8 +788,9 @@ def test_capped_scores_without_allocation_are_those_with_a_workspace(A, steps):
         assert bool(torch.isfinite(want).all()) and torch.equal(got, want) and torch.equal(also, esc)
 
 
-def test_a_captured_pass_on_the_8bit_cache_replays(A):
-    w = W.Workload("kv8", W.TINY, 3, (100, 900), ("uniform", 1, 4), "shuffled", "prefill", 0.0, ("const", 0.0), 778)
+@pytest.mark.parametrize("least,most", [(1, 4), (20, 40)])
+def test_a_captured_pass_on_the_8bit_cache_replays(A, least, most):
+    w = W.Workload("kv8", W.TINY, 3, (100, 900), ("uniform", least, most), "shuffled", "prefill", 0.0, ("const", 0.0), 778)
     batch, weights, gains, model, kv, db = _forward_session(A, w, 4, 30.0, True)
     A.arb_prefill(model, kv, H().prompt_batch(w, batch))
     ws = torch.empty(model.workspace_bytes(batch.batch, batch.total_tokens, db.max_ctx), dtype=torch.uint8, device="cuda")
