@@ -641,6 +641,15 @@ static AttnPlan plan_of_chunk(int batch, const int32_t *prefix_host, const int32
   return pl;
 }
 
+static long long first_chunk(long long keys_streamed, int max_ctx, int max_rows) {
+  const int cap = max_rows <= 32 ? kMaxChunkDecode : kMaxChunk;
+  long long chunk = (keys_streamed / kTargetWorkgroups + KT - 1) / KT * KT;
+  if (chunk > cap) chunk = cap;
+  if (chunk < kMinChunk) chunk = kMinChunk;
+  while (max_ctx > chunk * kMaxSplits) chunk += KT;
+  return chunk;
+}
+
 AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim) {
   long long keys_streamed = 0;          // sum over (sequence, kv head, query tile) of the context length
   int max_ctx = 0, max_step = 0;
@@ -653,11 +662,7 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
   // Keys per split, a first choice: about kTargetWorkgroups workgroups, never more than kMaxChunk keys (a batch whose steps all fit one
   // wave only streams the cache: there a longer chunk wins).  A sequence is cut into equal parts of at most that many keys
   // (attn_seq_chunk).  It bounds the splits, and with them the scratch of a call.
-  const int cap = max_step * G <= 32 ? kMaxChunkDecode : kMaxChunk;
-  long long chunk = (keys_streamed / kTargetWorkgroups + KT - 1) / KT * KT;
-  if (chunk > cap) chunk = cap;
-  if (chunk < kMinChunk) chunk = kMinChunk;
-  while (max_ctx > chunk * kMaxSplits) chunk += KT;
+  long long chunk = first_chunk(keys_streamed, max_ctx, max_step * G);
   // Then the chunk with the least estimated time among those that need no more splits, if it promises 3 %.  What the first choice does
   // not see: sequences of different lengths cut by one size make a quarter more items than there are places, or leave
   // a quarter of them empty, and a CU's two places share its pipes.  (Measured, first choice -> this, us of one layer: 1.5B shape,
@@ -686,6 +691,45 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
   return plan_of_chunk(batch, prefix_host, cu_host, G, n_kv_heads, (int)chunk, max_ctx, max_step);
 }
 
+// plan_us for the 8-bit and the capped forms where some step has more than 64 rows: the same sum with figures of their own, and with a step
+// where another round of workgroups begins, which plan_us has not: 20 % more workgroups than places are 10 to 30 % slower than 10 %
+// fewer.  Fitted to 34 batches (2 to 64 sequences, 600 to 32 K keys, steps of 6 to 150, five head layouts) x 13 chunks; over 169 batches, 26
+// of them among those, the launches are 3.1 % faster than with the chunk that plan_us picks (geometric mean; at best 36 %, at worst 24 % slower).
+static double fine_us(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim, int chunk) {
+  const double f = head_dim == 128 ? 1.0 : 0.53, item = 5.0, hidden = 0.2, places = kTargetWorkgroups, cus = kTargetWorkgroups / 2;
+  double n = 0, work = 0, tiles_all = 0, parts = 0, bytes = 0, shortest = 1e30, alone = 0, shared = 0;
+  const double per_chunk = 1.0 / chunk;
+  int max_ctx = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s, ns = 1 + (int)((ctx - 1) * per_chunk);
+    const bool few = (long long)s * G <= 32;
+    const double count = (double)ns * ceil_div(s * G, QROWS) * n_kv_heads, tiles = 1 + (int)((ctx - 1) / (double)(ns * KT));
+    const double per = (few ? 1.96 : 1.24) * f, by_itself = (few ? 1.94 : 1.75) * f;
+    n += count;
+    work += count * (tiles * per + item * hidden);
+    tiles_all += count * tiles;
+    parts += (double)ns * s * G * n_kv_heads;
+    bytes += (double)ctx * n_kv_heads * head_dim * 2;
+    shortest = tiles < shortest ? tiles : shortest;
+    alone = fmax(alone, tiles * by_itself);
+    shared = fmax(shared, tiles * per);
+    max_ctx = ctx > max_ctx ? ctx : max_ctx;
+  }
+  const double second = n <= cus ? 0 : 1.24 * f * (shortest + (tiles_all / n - shortest) * fmin(1.0, (n - cus) / cus));
+  double us;
+  if (n <= places) {
+    us = item + fmax(alone, shared + second);
+    if (n > 0.75 * places && n < 0.98 * places) us *= 1 + 0.22 * (n - 0.75 * places) / (0.25 * places);
+  } else {
+    const double round = item + 2 * work / n, last = item + 1.75 * f * tiles_all / n, full = floor(n / places), rest = n - full * places;
+    const double step = item + full * round + (rest == 0 ? 0 : rest <= cus ? last : last + (round - last) * (rest - cus) / cus);
+    us = 0.6 * fmax(item + alone, work / cus + 0.5 * work / n) + 0.4 * step;
+  }
+  us = fmax(us, item + bytes / 4.1e6);
+  const int splits = ceil_div(max_ctx, chunk);
+  return splits > 1 ? us + 7.2 + 0.5 * ceil_div(splits, 8) + parts * head_dim * 4.7e-7 : us;
+}
+
 // Few workgroups, contexts of more than kMinChunk keys: the launch is the latency of one part, and a tile (1.4 us) costs more than
 // another part does in the merge.  Parts of 64 keys where eight of them do (one round of the merge), otherwise of 128 or more, at most
 // kFineSplits, and no more workgroups than there are CUs: two of them on a CU would share its pipes, and the merge grows.
@@ -707,8 +751,24 @@ AttnPlan plan_attention_fine(int batch, const int32_t *prefix_host, const int32_
   if (chunk < least) chunk = least;
   while (max_ctx > chunk * kFineSplits) chunk += KT;
   if (max_ctx <= kMinChunk || chunk >= kMinChunk ||
-      (long long)cu_host[batch] * G * n_kv_heads * ceil_div(max_ctx, (int)chunk) > kFineRows)
-    return plan_attention(batch, prefix_host, cu_host, G, n_kv_heads, head_dim);
+      (long long)cu_host[batch] * G * n_kv_heads * ceil_div(max_ctx, (int)chunk) > kFineRows) {
+    if (max_step <= 64 / G) return plan_attention(batch, prefix_host, cu_host, G, n_kv_heads, head_dim);
+    // Enough workgroups: of the first choice and these, the chunk with the least estimated time (as plan_attention, but with more parts
+    // than the first choice if they pay: arb_workspace_bytes has room for parts of kMinChunk).
+    chunk = first_chunk(keys_streamed, max_ctx, max_step * G);
+    double best = chunk > kMinChunk || ceil_div(max_ctx, (int)chunk) > 8 ? fine_us(batch, prefix_host, cu_host, G, n_kv_heads, head_dim, (int)chunk) : 0.0;
+    if (best >= kReplanUs) {
+      best *= 0.97;
+      for (const int c : {256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 2560, 4096, 6144, 8192}) {
+        if (ceil_div(max_ctx, c) > kMaxSplits || c >= 2 * max_ctx) continue;
+        const double us = fine_us(batch, prefix_host, cu_host, G, n_kv_heads, head_dim, c);
+        if (us < best) {
+          best = us;
+          chunk = c;
+        }
+      }
+    }
+  }
   return plan_of_chunk(batch, prefix_host, cu_host, G, n_kv_heads, (int)chunk, max_ctx, max_step);
 }
 
