@@ -245,15 +245,16 @@ __device__ __forceinline__ void store_16_e4m3(const u32x4 &v, uint32_t scale_byt
 // of their own, and meet at the end; otherwise two of the four waves would only load.  (8B shape, 32 steps of 9 against 4 K to 32 K keys,
 // 8 bits: 355 -> 274 us, capped 448 -> 324, capped over bf16 436 -> 398; 32 of 18 to 32 against 1 K to 16 K, 4/2 heads of 64: 49 -> 34; a few short
 // contexts 0 to 7 % faster.)
+// The arguments that only the 8-bit and the capped forms take are the last ones: the others fit two lines of 64 bytes, and one word of a third
+// on the way to the first load of keys is a miss more (one token on 1531 keys 8.35 -> 8.72 us).
 template <int HD, bool SPLIT, bool PRESCALED, bool KV8, bool CAP, bool PAIRED>
 __global__ __launch_bounds__(256, 2) void attention_kernel(
     const bf16 *__restrict__ q, int q_row_stride, const void *__restrict__ k_pool, const void *__restrict__ v_pool,
-    const uint8_t *__restrict__ k_scale, const uint8_t *__restrict__ v_scale, float cap_out,
     const int32_t *__restrict__ block_tables, int max_blocks, const int32_t *__restrict__ prefix_lens,
     const int32_t *__restrict__ cu, int max_qtiles, int max_splits, int kv_chunk, const AttnItem *__restrict__ items,
     int n_items, int run, int T,
     int Hq, int Hkv, float scale_log2, bf16 *__restrict__ out, bf16 *__restrict__ part_acc, float *__restrict__ part_ml,
-    int32_t *__restrict__ tok_splits) {
+    int32_t *__restrict__ tok_splits, const uint8_t *__restrict__ k_scale, const uint8_t *__restrict__ v_scale, float cap_out) {
   constexpr int CPK = KV8 ? HD / 16 : HD / 8;   // 16-byte chunks per key of the cache
   constexpr int LOADS = KT * CPK / 256;    // wave-wide 1 KB loads per wave, operand and tile
   constexpr int KPL = 64 / CPK;            // keys covered by one wave-wide load (4 or 8: inside one block)
@@ -301,25 +302,20 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   const int row_wave = PAIRED ? wave & 1 : wave;
   const bool wave_active = row0 + row_wave * 32 < rows;   // waves past the last row only help with the loads
 
-  // this lane's query row
-  const int row = row0 + row_wave * 32 + col;
+  // This lane's query row.  Lanes behind the last row repeat it (the wave that has them has it too, so that they change no decision
+  // of the wave's): loads without conditions, eight in a row.  (With the assumption below: one token on 1531 keys 8.5 -> 8.0 us, 16 of the 8B
+  // shape on 2000 26.0 -> 25.4.)
+  const int row = row0 + row_wave * 32 + col, row_in = min(row, rows - 1);
   const bool row_ok = row < rows;
-  const int tok_i = row_ok ? row / G : 0;
-  const int head = hk * G + (row_ok ? row - tok_i * G : 0);
+  const int tok_i = row_in / G;
+  const int head = hk * G + row_in - tok_i * G;
   const int limit = p + tok_i;                         // last visible key (inclusive)
 
   bf16x8 qf[KSTEPS];
   {
     const bf16 *qrow = q + (size_t)(tok0 + tok_i) * q_row_stride + head * HD;
 #pragma unroll
-    for (int kk = 0; kk < KSTEPS; ++kk) {
-      if (row_ok) {
-        qf[kk] = *(const bf16x8 *)(qrow + kk * 16 + half * 8);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qf[kk][e] = (bf16)0.f;
-      }
-    }
+    for (int kk = 0; kk < KSTEPS; ++kk) qf[kk] = *(const bf16x8 *)(qrow + kk * 16 + half * 8);
   }
 
   f32x16 o[MT];
@@ -341,6 +337,10 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int last_key = ctx - 1, last_blk = last_key / ARB_KV_BLOCK;
   const int n_tiles = (kv_end - kv_begin + KT - 1) / KT;
+  // An item has a visible key.  Without knowing it the compiler moves the loads of the queries behind the first barrier, which costs (above)
+  // but in the 8-bit form of more than 64 rows, where the first tile's conversion then does not wait for them (16 steps of 64 on 2048 keys
+  // 33.1 -> 32.1 us).
+  if (!KV8 || PAIRED) __builtin_assume(n_tiles > 0);
   const int lkey = lane / CPK, pchunk = lane % CPK;
   int blk_id[LOADS];                       // pool block of each load of the tile to be issued next
   const unsigned first_blk = (unsigned)kv_begin / ARB_KV_BLOCK + (unsigned)(wave_u * KPL) / ARB_KV_BLOCK;
@@ -480,8 +480,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   }
 
   // The wave's result, row-major through the LDS (the stages are free: every tile ends with a barrier), so that a store writes whole
-  // rows; straight from the accumulators it is 16-byte pieces of 32 rows.  Chunks are swizzled by the row.  A few rows (one token
-  // of up to 15 heads a group) go straight: there the detour is 0.6 us of a short chain and saves nothing.
+  // rows; straight from the accumulators it is 16-byte pieces of 32 rows.  Chunks are swizzled by the row.  Where one wave has all the
+  // rows of its tile they go straight: the detour is 0.5 us of a short chain and saves nothing (30 rows of 16 sequences on 2048 keys 13.4 -> 12.8
+  // us, 32 of 8 on 2000 14.5 -> 14.0; with 48 and 60 rows no difference, with 64 rows on 8 sequences 19.35 -> 19.6).
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
   const size_t orow = (size_t)(tok0 + tok_i) * Hq + head;   // (token, head) index
   if (!wave_active) return;
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
     }
     return RELATIVE ? __builtin_bit_cast(bf16x4, h) : v;
   };
-  if (__builtin_amdgcn_readfirstlane(rows_here) < 16) {
+  if (rows - row0 <= 32) {
     if (row_ok) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -827,9 +828,10 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   const bool paired = max_rows <= 64;                      // (8-bit and capped forms only: the others keep the order of their sums)
 #define ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, PAIRED)                                                          \
   hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE, KV8, CAP, PAIRED>), grid, block, 0, st, q, q_row_stride, cache.k_pool, \
-                     cache.v_pool, cache.k_scale, cache.v_scale, cap_out, block_tables, max_blocks_per_seq, prefix_lens, \
+                     cache.v_pool, block_tables, max_blocks_per_seq, prefix_lens, \
                      cu_step_lens, plan.max_qtiles, plan.max_splits, plan.kv_chunk, lists.items, n_items, run, total_tokens, \
-                     n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml, count_splits ? lists.tok_splits : nullptr)
+                     n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml, count_splits ? lists.tok_splits : nullptr, \
+                     cache.k_scale, cache.v_scale, cap_out)
 #define ARB_ATTN_WAVES(HD, SPLIT, PRE, KV8, CAP)                                                                   \
   if (paired) ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, true); else ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, false)
 #define ARB_ATTN_FORM(HD, SPLIT)                                                                                   \
