@@ -362,7 +362,9 @@ int32_t arb_gemm_large_tile_columns(int32_t M, int32_t N, int32_t K, int32_t epi
  * [Hq, hd], already rotated; the pools already hold the step's keys/values.  out: bf16 [T, Hq*hd].
  * q_scaled == 0: q is the rotated query itself and the logits are q.k / sqrt(hd).  q_scaled != 0: q already
  * carries the factor log2(e) / sqrt(hd), as the forward's rotary stage stores it (multiplied in fp32 before
- * the one rounding to bf16), and q.k is taken as the logit in log2 units: the kernel of the forward. */
+ * the one rounding to bf16), and q.k is taken as the logit in log2 units: the kernel of the forward.
+ * Here and in the passes, more than about 2^31 (token, query head) rows or 2^24 workgroups in a call are refused (ARB_EUNSUPPORTED); with
+ * less workspace than arb_workspace_bytes the latter are the product of batch, parts, kv heads and query tiles of the longest step. */
 arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
                                const void *k_pool, const void *v_pool, const arb_batch *batch, void *out, void *ws,
                                size_t ws_bytes, void *stream);

@@ -332,6 +332,7 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
       if (arb_status s = check_layer(kv.layer(l), "8-bit cache")) return s;
   }
   const int T = bt->total_tokens, B = bt->batch, d = c.d_model;
+  if (arb_status s = check_attention_rows(T, c.n_q_heads)) return s;
   const int G = c.n_q_heads / c.n_kv_heads;
   const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
   const bool few_rows = attention_few_takes(attn_cache(kv.layer(l0), m->softcap), c.head_dim, max_rows);
@@ -353,6 +354,7 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
     return arb_fail(ARB_ECAPACITY, "arb_score_steps_noalloc: this batch needs %zu bytes of scratch but the static buffer "
                     "holds %zu (ARB_NOALLOC_SCRATCH_BYTES); use arb_score_steps with a workspace", w.total, ws_bytes);
   if (!ws || ws_bytes < w.total) return arb_fail(ARB_ECAPACITY, "workspace %zu < %zu bytes", ws_bytes, w.total);
+  if (arb_status s = few_rows ? check_attention_few(few_plan) : check_attention_launch(plan, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim)) return s;
   if (m->debug_ids) {
     // Debug mode (environment variable ARB_DEBUG_IDS at arb_model_create): the ids the kernels would
     // index with are range-checked on the device first, and this call waits for the verdict, so that a
@@ -779,6 +781,7 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
   if (q_row_stride < c.n_q_heads * c.head_dim || q_row_stride % 8 != 0)
     return arb_fail(ARB_EINVAL, "%s: q_row_stride %d", name, q_row_stride);
   const int G = c.n_q_heads / c.n_kv_heads, T = batch->total_tokens;
+  if (arb_status s = check_attention_rows(T, c.n_q_heads)) return s;
   const int max_rows = info.max_step > (1 << 20) ? 1 << 30 : info.max_step * G;
   if (attention_few_takes(cache, c.head_dim, max_rows)) {
     const FewPlan plan = plan_attention_few(batch->batch, batch->prefix_lens_host, batch->cu_step_lens_host, c.n_kv_heads, c.head_dim, max_rows, cache.k_scale != nullptr);
@@ -798,6 +801,7 @@ static arb_status stage_attention(const char *name, const arb_model *m, const vo
     plan.n_items = 0;
   const size_t need = plan.max_splits > 1 || plan.n_items > 0 ? attention_ws_bytes(plan.max_splits, plan.n_items, T, c.n_q_heads, c.head_dim) : 0;
   if (need > 0 && (!ws || ws_bytes < need)) return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
+  if (arb_status s = check_attention_launch(plan, batch->batch, T, c.n_q_heads, c.n_kv_heads, c.head_dim)) return s;
   if (plan.n_items > 0)                                    // without a list the attention launch counts the tokens' splits by itself
     if (arb_status s = launch_token_meta(batch->prefix_lens, batch->cu_step_lens, batch->block_tables, batch->batch, T,
                                          batch->max_blocks_per_seq, c.kv_block, nullptr, nullptr, st, &plan,

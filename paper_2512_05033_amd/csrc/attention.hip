@@ -578,6 +578,8 @@ static const int kMinChunk = 256, kMaxChunk = 4096, kMaxChunkDecode = 6144, kMax
 static const double kReplanUs = 20;
 static const int kFineSplits = 32;
 static const long long kFineRows = 65536;    // most rows of partial results in a plan of finer parts: 128 each for twice the CUs
+static const long long kMostGroups = 1 << 24;                // a launch has fewer than 2^32 threads
+static const long long kMostRows = 0x7fffffff - 2 * QROWS;   // query rows are counted in 32 bits, in whole tiles
 static const int kMaxRun = 16;                // longest run of work items on one XCD when there are few runs per XCD
 
 float attention_q_scale(int head_dim) { return (float)(1.4426950408889634 / sqrt((double)head_dim)); }
@@ -633,12 +635,13 @@ static AttnPlan plan_of_chunk(int batch, const int32_t *prefix_host, const int32
   pl.max_qtiles = ceil_div(max_step * G, QROWS);
   pl.kv_chunk = chunk;
   pl.max_splits = max_ctx > 0 ? ceil_div(max_ctx, pl.kv_chunk) : 1;
-  pl.n_items = 0;
+  long long items = 0;
   for (int b = 0; b < batch; ++b) {
     const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s, c = attn_seq_chunk(ctx, pl.kv_chunk);
     for (int begin = 0; begin < ctx; begin += c)
-      pl.n_items += (ceil_div(s * G, QROWS) - attn_first_qtile(prefix_host[b], G, begin)) * n_kv_heads;
+      items += (long long)(ceil_div(s * G, QROWS) - attn_first_qtile(prefix_host[b], G, begin)) * n_kv_heads;
   }
+  pl.n_items = items < 0x7fffffff ? (int)items : 0x7fffffff;
   return pl;
 }
 
@@ -803,6 +806,29 @@ AttnLists attention_lists(void *ws, const AttnPlan &plan, int total_tokens, int 
   return AttnLists{plan.n_items > 0 ? (AttnItem *)(p + align_up((size_t)total_tokens * sizeof(int32_t), 256)) : nullptr, (int32_t *)p};
 }
 
+arb_status check_attention_rows(int total_tokens, int n_q_heads) {
+  if ((long long)total_tokens * n_q_heads < kMostRows) return ARB_OK;
+  return arb_fail(ARB_EUNSUPPORTED, "attention: %d tokens of %d query heads in one call", total_tokens, n_q_heads);
+}
+
+// The launch's places: items of the list, or the product that is searched without one.
+static long long attention_places(const AttnPlan &plan, int batch, int n_kv_heads) {
+  return plan.n_items > 0 ? plan.n_items : (long long)batch * plan.max_splits * n_kv_heads * plan.max_qtiles;
+}
+// A run is a group's query tiles, shortened where so few of them fit that some XCDs would get a whole run more.
+static int attention_run(const AttnPlan &plan, long long places) {
+  const int run = plan.max_qtiles;
+  return run > kMaxRun && places % (8LL * run) != 0 && places < 4 * 8LL * run ? kMaxRun : run;
+}
+static long long attention_groups(long long places, int run) { return (places + 8LL * run - 1) / (8LL * run) * (8LL * run); }
+
+arb_status check_attention_launch(const AttnPlan &plan, int batch, int total_tokens, int n_q_heads, int n_kv_heads, int head_dim) {
+  const long long places = attention_places(plan, batch, n_kv_heads), groups = attention_groups(places, attention_run(plan, places));
+  const long long merge = plan.max_splits > 1 ? (long long)total_tokens * n_q_heads / (2048 / head_dim) + 1 : 0;
+  if (groups < kMostGroups && merge < kMostGroups) return ARB_OK;
+  return arb_fail(ARB_EUNSUPPORTED, "attention: %lld workgroups in one call", groups > merge ? groups : merge);
+}
+
 arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &cache,
                             const int32_t *block_tables, int max_blocks_per_seq, int batch, int total_tokens, int n_q_heads,
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
@@ -813,7 +839,8 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   const bool split = plan.max_splits > 1, listed = plan.n_items > 0;
   if ((split || listed) && (!ws || ws_bytes < need))
     return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
-  const int n_items = listed ? plan.n_items : batch * plan.max_splits * n_kv_heads * plan.max_qtiles;
+  if (arb_status s = check_attention_launch(plan, batch, total_tokens, n_q_heads, n_kv_heads, head_dim)) return s;
+  const int n_items = (int)attention_places(plan, batch, n_kv_heads), run = attention_run(plan, n_items);
   bf16 *part_acc = (bf16 *)ws;
   float *part_ml = (float *)((char *)ws + part_acc_bytes(plan.max_splits, total_tokens, n_q_heads, head_dim));
   const AttnLists lists = split || listed ? attention_lists(ws, plan, total_tokens, n_q_heads, head_dim) : AttnLists{};
@@ -821,10 +848,7 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   const bool kv8 = cache.k_scale != nullptr, capped = cache.softcap > 0.f;
   const float to_log2 = q_prescaled ? 1.0f : attention_q_scale(head_dim);
   const float scale_log2 = capped ? 2.0f * to_log2 / cache.softcap : to_log2, cap_out = capped ? 1.44269504f * cache.softcap : 0.f;
-  // A run is a group's query tiles, shortened where so few of them fit that some XCDs would get a whole run more.
-  int run = plan.max_qtiles;
-  if (run > kMaxRun && n_items % (8 * run) != 0 && n_items < 4 * 8 * run) run = kMaxRun;
-  const dim3 grid(ceil_div(n_items, 8 * run) * 8 * run), block(256);
+  const dim3 grid((unsigned)attention_groups(n_items, run)), block(256);
   const bool paired = max_rows <= 64;                      // (8-bit and capped forms only: the others keep the order of their sums)
 #define ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, PAIRED)                                                          \
   hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE, KV8, CAP, PAIRED>), grid, block, 0, st, q, q_row_stride, cache.k_pool, \

@@ -165,6 +165,10 @@ struct AttnCache {
   const uint8_t *k_scale, *v_scale;
   float softcap;
 };
+// Refusals of what the kernels' counts and the launches do not hold, for callers that enqueue something first: the first one before a
+// plan is made, the second one for the plan that is launched.
+arb_status check_attention_rows(int total_tokens, int n_q_heads);
+arb_status check_attention_launch(const AttnPlan &plan, int batch, int total_tokens, int n_q_heads, int n_kv_heads, int head_dim);
 arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &cache,
                             const int32_t *block_tables, int max_blocks_per_seq, int batch, int total_tokens, int n_q_heads,
                             int n_kv_heads, int head_dim, const AttnPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
@@ -181,6 +185,7 @@ bool attention_few_takes(const AttnCache &cache, int head_dim, int max_rows);
 size_t attention_few_ws_bytes(int parts, int total_tokens, int n_q_heads, int head_dim);
 int attention_few_parts_cap(int max_ctx);   // largest `parts` for contexts <= max_ctx
 FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t *cu_host, int n_kv_heads, int head_dim, int max_rows, bool kv8);
+arb_status check_attention_few(const FewPlan &plan);
 arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache &cache, const int32_t *block_tables,
                                 int max_blocks_per_seq, int batch, int total_tokens, int max_rows, int n_q_heads, int n_kv_heads,
                                 int head_dim, const FewPlan &plan, bf16 *out, void *ws, size_t ws_bytes,
