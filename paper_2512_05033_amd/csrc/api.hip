@@ -354,7 +354,7 @@ static arb_status forward(arb_model *m, const CacheTables &kv, const arb_batch *
     return arb_fail(ARB_ECAPACITY, "arb_score_steps_noalloc: this batch needs %zu bytes of scratch but the static buffer "
                     "holds %zu (ARB_NOALLOC_SCRATCH_BYTES); use arb_score_steps with a workspace", w.total, ws_bytes);
   if (!ws || ws_bytes < w.total) return arb_fail(ARB_ECAPACITY, "workspace %zu < %zu bytes", ws_bytes, w.total);
-  if (arb_status s = few_rows ? check_attention_few(few_plan) : check_attention_launch(plan, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim)) return s;
+  if (arb_status s = few_rows ? check_attention_few(few_plan, B, c.n_kv_heads) : check_attention_launch(plan, B, T, c.n_q_heads, c.n_kv_heads, c.head_dim)) return s;
   if (m->debug_ids) {
     // Debug mode (environment variable ARB_DEBUG_IDS at arb_model_create): the ids the kernels would
     // index with are range-checked on the device first, and this call waits for the verdict, so that a

@@ -520,8 +520,9 @@ FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t 
   return FewPlan{(int)per, 1, most_parts(most, (int)per), (total + per - 1) / per, total};
 }
 
-arb_status check_attention_few(const FewPlan &plan) {
-  if (plan.tiles + plan.per <= 0x7fffffffLL && plan.groups < 1 << 24) return ARB_OK;
+arb_status check_attention_few(const FewPlan &plan, int batch, int n_kv_heads) {
+  const long long merges = plan.parts > 1 ? (long long)batch * n_kv_heads : 0;
+  if (plan.tiles + plan.per <= 0x7fffffffLL && plan.groups < 1 << 24 && merges < 1 << 24) return ARB_OK;
   return arb_fail(ARB_EUNSUPPORTED, "attention: %lld tiles of keys in one call", plan.tiles);
 }
 
@@ -533,7 +534,7 @@ arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache
   const bool split = plan.parts > 1, capped = cache.softcap > 0.f;
   const size_t need = attention_few_ws_bytes(plan.parts, total_tokens, n_q_heads, head_dim);
   if (split && (!ws || ws_bytes < need)) return arb_fail(ARB_ECAPACITY, "attention: workspace %zu < %zu bytes", ws_bytes, need);
-  if (arb_status s = check_attention_few(plan)) return s;
+  if (arb_status s = check_attention_few(plan, batch, n_kv_heads)) return s;
   const float to_log2 = q_prescaled ? 1.0f : attention_q_scale(head_dim);
   FewArgs a{q, q_row_stride, (const uint8_t *)cache.k_pool, (const uint8_t *)cache.v_pool, cache.k_scale, cache.v_scale,
             block_tables, prefix_lens, cu_step_lens, batch, max_blocks_per_seq, plan.parts, plan.per, plan.in_a_row, total_tokens, n_q_heads,

@@ -185,7 +185,7 @@ bool attention_few_takes(const AttnCache &cache, int head_dim, int max_rows);
 size_t attention_few_ws_bytes(int parts, int total_tokens, int n_q_heads, int head_dim);
 int attention_few_parts_cap(int max_ctx);   // largest `parts` for contexts <= max_ctx
 FewPlan plan_attention_few(int batch, const int32_t *prefix_host, const int32_t *cu_host, int n_kv_heads, int head_dim, int max_rows, bool kv8);
-arb_status check_attention_few(const FewPlan &plan);
+arb_status check_attention_few(const FewPlan &plan, int batch, int n_kv_heads);
 arb_status launch_attention_few(const bf16 *q, int q_row_stride, const AttnCache &cache, const int32_t *block_tables,
                                 int max_blocks_per_seq, int batch, int total_tokens, int max_rows, int n_q_heads, int n_kv_heads,
                                 int head_dim, const FewPlan &plan, bf16 *out, void *ws, size_t ws_bytes,

@@ -85,4 +85,10 @@ def test_the_border_of_a_launch(lib):
     assert check(n_items=0x7fffffff) == B.ARB_EUNSUPPORTED
     assert check(batch=(1 << 21) - 1) == B.ARB_OK and check(batch=1 << 21) == B.ARB_EUNSUPPORTED
     assert check(batch=1 << 16, max_qtiles=1 << 13) == B.ARB_EUNSUPPORTED        # 2^32
+    from helpers import FewPlan
+    g = lib._Z19check_attention_fewRK7FewPlanii
+    g.restype, g.argtypes = C.c_int, [C.POINTER(FewPlan), C.c_int, C.c_int]
+    few = lambda batch, **plan: g(C.byref(FewPlan(**{"per": 8, "in_a_row": 1, "parts": 2, "groups": 512, "tiles": 1 << 20, **plan})), batch, 8)
+    assert few((1 << 21) - 1) == B.ARB_OK and few(1 << 21) == B.ARB_EUNSUPPORTED and few(1 << 21, parts=1) == B.ARB_OK    # a merge a pair
+    assert few(1, groups=1 << 24) == B.ARB_EUNSUPPORTED and few(1, tiles=0x7fffffff) == B.ARB_EUNSUPPORTED
     assert check(tokens=1 << 24) == B.ARB_OK and check(tokens=1 << 24, max_splits=2) == B.ARB_EUNSUPPORTED   # the merge: 32 rows a workgroup
