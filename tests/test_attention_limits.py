@@ -92,3 +92,18 @@ def test_the_border_of_a_launch(lib):
     assert few((1 << 21) - 1) == B.ARB_OK and few(1 << 21) == B.ARB_EUNSUPPORTED and few(1 << 21, parts=1) == B.ARB_OK    # a merge a pair
     assert few(1, groups=1 << 24) == B.ARB_EUNSUPPORTED and few(1, tiles=0x7fffffff) == B.ARB_EUNSUPPORTED
     assert check(tokens=1 << 24) == B.ARB_OK and check(tokens=1 << 24, max_splits=2) == B.ARB_EUNSUPPORTED   # the merge: 32 rows a workgroup
+
+
+# The two batches that the static array of arb_score_steps_noalloc is said to hold, with capped scores too, however many sequences they are.
+@pytest.mark.parametrize("softcap", [0.0, 30.0])
+@pytest.mark.parametrize("shape,tokens,ctx", [
+    (dict(d_model=1536, n_q_heads=12, n_kv_heads=2, head_dim=128, d_ffn=8960), 128, 32768),
+    (dict(d_model=4096, n_q_heads=32, n_kv_heads=8, head_dim=128, d_ffn=14336), 64, 8192)])
+def test_the_static_array_holds_the_batches_that_are_promised(lib, shape, tokens, ctx, softcap):
+    from paper_2512_05033_amd import binding as B
+    w, _keep = _weights()
+    _, h = _create(lib, _cfg(**shape), w)
+    assert lib.arb_model_set_softcap(h, softcap) == B.ARB_OK
+    for batch in range(1, tokens + 1):
+        assert lib.arb_workspace_bytes(h, batch, tokens, ctx) <= B.NOALLOC_SCRATCH_BYTES
+    lib.arb_model_destroy(h)
