@@ -590,13 +590,29 @@ int attention_splits_cap(int max_ctx) {
   return n < kMaxSplits ? n : kMaxSplits;
 }
 
-// Estimated time of an attention launch and its merge with parts of at most `chunk` keys.  A 64-key tile of 128 rows takes 1.4 us
-// alone on a CU and 1.15 us of the CU's time when two workgroups share it, one of a few rows (one wave works) 2.3 and 1.5; an item costs 4 us
-// more, half of it not hidden by its neighbour.  With more items than places the launch ends half an item after the average place.  Between three
+// Estimated time of an attention launch and its merge with parts of at most `chunk` keys.  A 64-key tile of 128 rows takes `tile_alone` alone on
+// a CU and `tile` of the CU's time when two workgroups share it, one of a few rows (one wave works) tile_alone_few and tile_few; an item costs
+// `item` more, of which its neighbour leaves `shown`.  With more items than places the launch ends half an item after the average place.  Between three
 // quarters and all of the places a launch takes up to a fifth longer than that: CUs that got two of the long items hold it up.
-// Fitted to 43 batches (1 to 64 sequences, 50 to 32 K keys, steps of 1 to 128, three shapes) x up to 17 chunks.
-static double plan_us(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim, int chunk) {
-  const double f = head_dim == 128 ? 1.0 : 0.6, item = 4.0, places = kTargetWorkgroups, cus = kTargetWorkgroups / 2;
+struct AttnCosts {
+  double tile, tile_few, tile_alone, tile_alone_few;       // us
+  double narrow;                                           // of these with heads of 64
+  double item, shown;
+  double second, second_few;                               // the tile of the items behind the first round; where all steps are of few rows
+  double rounds;                                           // how far the launch goes by whole rounds of workgroups, beyond all places
+  double element, rate;                                    // bytes per cache element, MB/s
+  double merge, merge_round, merge_element;
+};
+// The uncapped launch over bf16 pools.  Fitted to 43 batches (1 to 64 sequences, 50 to 32 K keys, steps of 1 to 128, three shapes) x up to 17 chunks.
+static const AttnCosts kPlainCosts = {1.15, 1.5, 1.4, 2.3, 0.6, 4.0, 0.5, 1.15, 1.5, 0.0, 4, 5.0e6, 5.0, 1.3, 4e-7};
+// The 8-bit and the capped forms where some step has more than 64 rows.  They go by rounds, which the others do not: 20 % more workgroups than
+// places are 10 to 30 % slower than 10 % fewer.  Fitted to 34 batches (2 to 64 sequences, 600 to 32 K keys, steps of 6 to 150, five head
+// layouts) x 13 chunks; over 169 batches, 26 of them among those, the launches are 3.1 % faster than with the chunk that the other figures
+// pick (geometric mean; at best 36 %, at worst 24 % slower).
+static const AttnCosts kFineCosts = {1.24, 1.96, 1.75, 1.94, 0.53, 5.0, 0.2, 1.24, 1.24, 0.4, 2, 4.1e6, 7.2, 0.5, 4.7e-7};
+
+static double plan_us(const AttnCosts &k, int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim, int chunk) {
+  const double f = head_dim == 128 ? 1.0 : k.narrow, places = kTargetWorkgroups, cus = kTargetWorkgroups / 2;
   double n = 0, work = 0, tiles_all = 0, parts = 0, bytes = 0, shortest = 1e30, alone = 0, shared = 0;
   const double per_chunk = 1.0 / chunk;
   int max_ctx = 0;
@@ -604,29 +620,34 @@ static double plan_us(int batch, const int32_t *prefix_host, const int32_t *cu_h
   for (int b = 0; b < batch; ++b) {                        // without integer divisions: some hundred of these per call
     const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s, ns = 1 + (int)((ctx - 1) * per_chunk);
     const bool few = (long long)s * G <= 32;
-    const double count = (double)ns * ceil_div(s * G, QROWS) * n_kv_heads, tiles = 1 + (int)((ctx - 1) / (double)(ns * KT)), per = few ? 1.5 : 1.15;
+    const double count = (double)ns * ceil_div(s * G, QROWS) * n_kv_heads, tiles = 1 + (int)((ctx - 1) / (double)(ns * KT)), per = few ? k.tile_few : k.tile;
     n += count;
-    work += count * (tiles * per * f + item / 2);
+    work += count * (tiles * per * f + k.item * k.shown);
     tiles_all += count * tiles;
     parts += (double)ns * s * G * n_kv_heads;
-    bytes += (double)ctx * n_kv_heads * head_dim * 4;
+    bytes += (double)ctx * n_kv_heads * head_dim * k.element;
     shortest = tiles < shortest ? tiles : shortest;
-    alone = fmax(alone, tiles * (few ? 2.3 : 1.4) * f);
+    alone = fmax(alone, tiles * (few ? k.tile_alone_few : k.tile_alone) * f);
     shared = fmax(shared, tiles * per * f);
     decode = decode && few;
     max_ctx = ctx > max_ctx ? ctx : max_ctx;
   }
-  const double second = n <= cus ? 0 : (decode ? 1.5 : 1.15) * f * (shortest + (tiles_all / n - shortest) * fmin(1.0, (n - cus) / cus));
+  const double second = n <= cus ? 0 : (decode ? k.second_few : k.second) * f * (shortest + (tiles_all / n - shortest) * fmin(1.0, (n - cus) / cus));
   double us;
   if (n <= places) {
-    us = item + fmax(alone, shared + second);
+    us = k.item + fmax(alone, shared + second);
     if (n > 0.75 * places && n < 0.98 * places) us *= 1 + 0.22 * (n - 0.75 * places) / (0.25 * places);
   } else {
-    us = fmax(item + alone, work / cus + 0.5 * work / n);
+    us = fmax(k.item + alone, work / cus + 0.5 * work / n);
+    if (k.rounds > 0) {
+      const double round = k.item + 2 * work / n, last = k.item + k.tile_alone * f * tiles_all / n, full = floor(n / places), rest = n - full * places;
+      const double step = k.item + full * round + (rest == 0 ? 0 : rest <= cus ? last : last + (round - last) * (rest - cus) / cus);
+      us = (1 - k.rounds) * us + k.rounds * step;
+    }
   }
-  us = fmax(us, item + bytes / 5.0e6);
+  us = fmax(us, k.item + bytes / k.rate);
   const int splits = ceil_div(max_ctx, chunk);
-  return splits > 1 ? us + 5.0 + 1.3 * ceil_div(splits, 8) + parts * head_dim * 4e-7 : us;
+  return splits > 1 ? us + k.merge + k.merge_round * ceil_div(splits, 8) + parts * head_dim * k.merge_element : us;
 }
 
 static AttnPlan plan_of_chunk(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int chunk,
@@ -678,13 +699,13 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
   // At most eight of the shortest parts (one round of the merge) stay: such a launch is the latency of one part.
   const int splits = max_ctx > 0 ? ceil_div(max_ctx, (int)chunk) : 1;
   // So does a choice of less than kReplanUs: the estimates themselves take some microseconds of the host, which a short pass waits for.
-  const double first = chunk > kMinChunk || splits > 8 ? plan_us(batch, prefix_host, cu_host, G, n_kv_heads, head_dim, (int)chunk) : 0.0;
+  const double first = chunk > kMinChunk || splits > 8 ? plan_us(kPlainCosts, batch, prefix_host, cu_host, G, n_kv_heads, head_dim, (int)chunk) : 0.0;
   if (first >= kReplanUs) {
     double best = 0.97 * first;
     long long pick = chunk;
     for (const int c : {256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 2560, 3072, 4096, 6144, 8192}) {
       if (ceil_div(max_ctx, c) > splits || c >= 2 * max_ctx) continue;
-      const double us = plan_us(batch, prefix_host, cu_host, G, n_kv_heads, head_dim, c);
+      const double us = plan_us(kPlainCosts, batch, prefix_host, cu_host, G, n_kv_heads, head_dim, c);
       if (us < best) {
         best = us;
         pick = c;
@@ -693,45 +714,6 @@ AttnPlan plan_attention(int batch, const int32_t *prefix_host, const int32_t *cu
     chunk = pick;
   }
   return plan_of_chunk(batch, prefix_host, cu_host, G, n_kv_heads, (int)chunk, max_ctx, max_step);
-}
-
-// plan_us for the 8-bit and the capped forms where some step has more than 64 rows: the same sum with figures of their own, and with a step
-// where another round of workgroups begins, which plan_us has not: 20 % more workgroups than places are 10 to 30 % slower than 10 %
-// fewer.  Fitted to 34 batches (2 to 64 sequences, 600 to 32 K keys, steps of 6 to 150, five head layouts) x 13 chunks; over 169 batches, 26
-// of them among those, the launches are 3.1 % faster than with the chunk that plan_us picks (geometric mean; at best 36 %, at worst 24 % slower).
-static double fine_us(int batch, const int32_t *prefix_host, const int32_t *cu_host, int G, int n_kv_heads, int head_dim, int chunk) {
-  const double f = head_dim == 128 ? 1.0 : 0.53, item = 5.0, hidden = 0.2, places = kTargetWorkgroups, cus = kTargetWorkgroups / 2;
-  double n = 0, work = 0, tiles_all = 0, parts = 0, bytes = 0, shortest = 1e30, alone = 0, shared = 0;
-  const double per_chunk = 1.0 / chunk;
-  int max_ctx = 0;
-  for (int b = 0; b < batch; ++b) {
-    const int s = cu_host[b + 1] - cu_host[b], ctx = prefix_host[b] + s, ns = 1 + (int)((ctx - 1) * per_chunk);
-    const bool few = (long long)s * G <= 32;
-    const double count = (double)ns * ceil_div(s * G, QROWS) * n_kv_heads, tiles = 1 + (int)((ctx - 1) / (double)(ns * KT));
-    const double per = (few ? 1.96 : 1.24) * f, by_itself = (few ? 1.94 : 1.75) * f;
-    n += count;
-    work += count * (tiles * per + item * hidden);
-    tiles_all += count * tiles;
-    parts += (double)ns * s * G * n_kv_heads;
-    bytes += (double)ctx * n_kv_heads * head_dim * 2;
-    shortest = tiles < shortest ? tiles : shortest;
-    alone = fmax(alone, tiles * by_itself);
-    shared = fmax(shared, tiles * per);
-    max_ctx = ctx > max_ctx ? ctx : max_ctx;
-  }
-  const double second = n <= cus ? 0 : 1.24 * f * (shortest + (tiles_all / n - shortest) * fmin(1.0, (n - cus) / cus));
-  double us;
-  if (n <= places) {
-    us = item + fmax(alone, shared + second);
-    if (n > 0.75 * places && n < 0.98 * places) us *= 1 + 0.22 * (n - 0.75 * places) / (0.25 * places);
-  } else {
-    const double round = item + 2 * work / n, last = item + 1.75 * f * tiles_all / n, full = floor(n / places), rest = n - full * places;
-    const double step = item + full * round + (rest == 0 ? 0 : rest <= cus ? last : last + (round - last) * (rest - cus) / cus);
-    us = 0.6 * fmax(item + alone, work / cus + 0.5 * work / n) + 0.4 * step;
-  }
-  us = fmax(us, item + bytes / 4.1e6);
-  const int splits = ceil_div(max_ctx, chunk);
-  return splits > 1 ? us + 7.2 + 0.5 * ceil_div(splits, 8) + parts * head_dim * 4.7e-7 : us;
 }
 
 // Few workgroups, contexts of more than kMinChunk keys: the launch is the latency of one part, and a tile (1.4 us) costs more than
@@ -760,12 +742,12 @@ AttnPlan plan_attention_fine(int batch, const int32_t *prefix_host, const int32_
     // Enough workgroups: of the first choice and these, the chunk with the least estimated time (as plan_attention, but with more parts
     // than the first choice if they pay: arb_workspace_bytes has room for parts of kMinChunk).
     chunk = first_chunk(keys_streamed, max_ctx, max_step * G);
-    double best = chunk > kMinChunk || ceil_div(max_ctx, (int)chunk) > 8 ? fine_us(batch, prefix_host, cu_host, G, n_kv_heads, head_dim, (int)chunk) : 0.0;
+    double best = chunk > kMinChunk || ceil_div(max_ctx, (int)chunk) > 8 ? plan_us(kFineCosts, batch, prefix_host, cu_host, G, n_kv_heads, head_dim, (int)chunk) : 0.0;
     if (best >= kReplanUs) {
       best *= 0.97;
       for (const int c : {256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 2560, 4096, 6144, 8192}) {
         if (ceil_div(max_ctx, c) > kMaxSplits || c >= 2 * max_ctx) continue;
-        const double us = fine_us(batch, prefix_host, cu_host, G, n_kv_heads, head_dim, c);
+        const double us = plan_us(kFineCosts, batch, prefix_host, cu_host, G, n_kv_heads, head_dim, c);
         if (us < best) {
           best = us;
           chunk = c;
