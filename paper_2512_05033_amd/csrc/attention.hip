@@ -241,13 +241,16 @@ __device__ __forceinline__ void store_16_e4m3(const u32x4 &v, uint32_t scale_byt
   *(bf16x8 *)chunk1 = b.c;
 }
 
-// PAIRED, where no step has more than 64 rows: waves w and w + 2 share 32 rows and take half a tile's keys each, with an online softmax
+// ROWS: no step has more rows of a kv head.  32, the uncapped bf16 forms: one wave has them all, and its results go out straight from the accumulators
+// (as they also do in the other forms where a tile has no more rows; a kernel without the detour through the LDS beside it
+// holds fewer registers: 16 tokens of the 8B shape on 513 to 1024 keys 11.25 -> 11.05 us).
+// 64, the 8-bit and the capped forms (PAIRED): waves w and w + 2 share 32 rows and take half a tile's keys each, with an online softmax
 // of their own, and meet at the end; otherwise two of the four waves would only load.  (8B shape, 32 steps of 9 against 4 K to 32 K keys,
 // 8 bits: 355 -> 274 us, capped 448 -> 324, capped over bf16 436 -> 398; 32 of 18 to 32 against 1 K to 16 K, 4/2 heads of 64: 49 -> 34; a few short
 // contexts 0 to 7 % faster.)
 // The arguments that only the 8-bit and the capped forms take are the last ones: the others fit two lines of 64 bytes, and one word of a third
 // on the way to the first load of keys is a miss more (one token on 1531 keys 8.35 -> 8.72 us).
-template <int HD, bool SPLIT, bool PRESCALED, bool KV8, bool CAP, bool PAIRED>
+template <int HD, bool SPLIT, bool PRESCALED, bool KV8, bool CAP, int ROWS>
 __global__ __launch_bounds__(256, 2) void attention_kernel(
     const bf16 *__restrict__ q, int q_row_stride, const void *__restrict__ k_pool, const void *__restrict__ v_pool,
     const int32_t *__restrict__ block_tables, int max_blocks, const int32_t *__restrict__ prefix_lens,
@@ -261,6 +264,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   constexpr int KSTEPS = HD / 16;          // MFMA k-steps over the head dimension
   constexpr int MT = HD / 32;              // 32-row tiles of O^T
   constexpr int EPC = KV8 ? 16 : 8, EB = KV8 ? 1 : 2;      // elements per chunk, bytes per element
+  constexpr bool PAIRED = ROWS == 64;
   // Two stages of K and V; one array per stage so that LDS reads of one stage are not ordered
   // behind the direct-to-LDS loads in flight into the other.
   __shared__ __attribute__((aligned(16))) bf16 K0[KT * HD], K1[KT * HD], V0[KT * HD], V1[KT * HD];
@@ -303,8 +307,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   const bool wave_active = row0 + row_wave * 32 < rows;   // waves past the last row only help with the loads
 
   // This lane's query row.  Lanes behind the last row repeat it (the wave that has them has it too, so that they change no decision
-  // of the wave's): loads without conditions, eight in a row.  (With the assumption below: one token on 1531 keys 8.5 -> 8.0 us, 16 of the 8B
-  // shape on 2000 26.0 -> 25.4.)
+  // of the wave's): loads without conditions of their own, eight in a row, and none by waves without rows.  (With the assumption below: one token on 1531
+  // keys 8.5 -> 7.9 us, 16 of the 8B shape on 2000 26.0 -> 25.5.)
   const int row = row0 + row_wave * 32 + col, row_in = min(row, rows - 1);
   const bool row_ok = row < rows;
   const int tok_i = row_in / G;
@@ -312,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   const int limit = p + tok_i;                         // last visible key (inclusive)
 
   bf16x8 qf[KSTEPS];
-  {
+  if (wave_active) {
     const bf16 *qrow = q + (size_t)(tok0 + tok_i) * q_row_stride + head * HD;
 #pragma unroll
     for (int kk = 0; kk < KSTEPS; ++kk) qf[kk] = *(const bf16x8 *)(qrow + kk * 16 + half * 8);
@@ -520,7 +524,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
     }
     return RELATIVE ? __builtin_bit_cast(bf16x4, h) : v;
   };
-  if (rows - row0 <= 32) {
+  if (ROWS == 32 || rows - row0 <= 32) {
     if (row_ok) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -831,26 +835,30 @@ arb_status launch_attention(const bf16 *q, int q_row_stride, const AttnCache &ca
   const float to_log2 = q_prescaled ? 1.0f : attention_q_scale(head_dim);
   const float scale_log2 = capped ? 2.0f * to_log2 / cache.softcap : to_log2, cap_out = capped ? 1.44269504f * cache.softcap : 0.f;
   const dim3 grid((unsigned)attention_groups(n_items, run)), block(256);
-  const bool paired = max_rows <= 64;                      // (8-bit and capped forms only: the others keep the order of their sums)
-#define ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, PAIRED)                                                          \
-  hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE, KV8, CAP, PAIRED>), grid, block, 0, st, q, q_row_stride, cache.k_pool, \
+  // (pairs of waves in the 8-bit and the capped forms only: the others keep the order of their sums)
+  const bool paired = max_rows <= 64, one_wave = max_rows <= 32;
+#define ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, ROWS)                                                            \
+  hipLaunchKernelGGL((attention_kernel<HD, SPLIT, PRE, KV8, CAP, ROWS>), grid, block, 0, st, q, q_row_stride, cache.k_pool, \
                      cache.v_pool, block_tables, max_blocks_per_seq, prefix_lens, \
                      cu_step_lens, plan.max_qtiles, plan.max_splits, plan.kv_chunk, lists.items, n_items, run, total_tokens, \
                      n_q_heads, n_kv_heads, scale_log2, out, part_acc, part_ml, count_splits ? lists.tok_splits : nullptr, \
                      cache.k_scale, cache.v_scale, cap_out)
-#define ARB_ATTN_WAVES(HD, SPLIT, PRE, KV8, CAP)                                                                   \
-  if (paired) ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, true); else ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, false)
+#define ARB_ATTN_FINE(HD, SPLIT, PRE, KV8, CAP)                                                                    \
+  if (paired) ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, 64); else ARB_ATTN_LAUNCH(HD, SPLIT, PRE, KV8, CAP, 128)
+#define ARB_ATTN_PLAIN(HD, SPLIT, PRE)                                                                             \
+  if (one_wave) ARB_ATTN_LAUNCH(HD, SPLIT, PRE, false, false, 32); else ARB_ATTN_LAUNCH(HD, SPLIT, PRE, false, false, 128)
 #define ARB_ATTN_FORM(HD, SPLIT)                                                                                   \
-  if (kv8 && capped) { ARB_ATTN_WAVES(HD, SPLIT, false, true, true); }                                             \
-  else if (capped) { ARB_ATTN_WAVES(HD, SPLIT, false, false, true); }                                              \
-  else if (kv8 && q_prescaled) { ARB_ATTN_WAVES(HD, SPLIT, true, true, false); }                                   \
-  else if (kv8) { ARB_ATTN_WAVES(HD, SPLIT, false, true, false); }                                                 \
-  else if (q_prescaled) ARB_ATTN_LAUNCH(HD, SPLIT, true, false, false, false);                                     \
-  else ARB_ATTN_LAUNCH(HD, SPLIT, false, false, false, false)
+  if (kv8 && capped) { ARB_ATTN_FINE(HD, SPLIT, false, true, true); }                                              \
+  else if (capped) { ARB_ATTN_FINE(HD, SPLIT, false, false, true); }                                               \
+  else if (kv8 && q_prescaled) { ARB_ATTN_FINE(HD, SPLIT, true, true, false); }                                    \
+  else if (kv8) { ARB_ATTN_FINE(HD, SPLIT, false, true, false); }                                                  \
+  else if (q_prescaled) { ARB_ATTN_PLAIN(HD, SPLIT, true); }                                                       \
+  else { ARB_ATTN_PLAIN(HD, SPLIT, false); }
   if (head_dim == 128) { if (split) { ARB_ATTN_FORM(128, true); } else { ARB_ATTN_FORM(128, false); } }
   else                 { if (split) { ARB_ATTN_FORM(64, true); } else { ARB_ATTN_FORM(64, false); } }
 #undef ARB_ATTN_FORM
-#undef ARB_ATTN_WAVES
+#undef ARB_ATTN_PLAIN
+#undef ARB_ATTN_FINE
 #undef ARB_ATTN_LAUNCH
   ARB_CHECK_LAUNCH("attention");
   if (split) {
