@@ -183,7 +183,8 @@ arb_status arb_model_set_softcap(arb_model *m, float softcap);
 
 /* Bytes of device workspace the hot calls need for batches of at most
  * max_total_tokens step tokens in at most max_batch sequences whose context
- * (prefix + step) is at most max_ctx tokens.  0 on invalid arguments. */
+ * (prefix + step) is at most max_ctx tokens, on either type of cache and with or without a cap.  0 on invalid arguments.
+ * A call takes any workspace that holds what its own batch needs, which on a bf16 cache without a cap may be half of it. */
 size_t arb_workspace_bytes(const arb_model *m, int32_t max_batch, int32_t max_total_tokens, int32_t max_ctx);
 
 /* The router forward (Section 4.2; Alg. 1 "routing decision") or, with
@@ -371,7 +372,9 @@ arb_status arb_stage_attention(const arb_model *m, const void *q, int32_t q_row_
 
 /* Append-attention of one layer over a cache of either type, with softcap as in arb_model_set_softcap (the argument counts, not the
  * model's).  The other arguments are those of arb_stage_attention, of which this is the general form; without a cap and over bf16
- * pools the results are its results.  A value of a bf16 pool that is not finite may reach every row of its step, also those that do
+ * pools the results are its results.  Over an 8-bit cache or with a cap, with more than 32 (token, query head) rows per kv head and a context
+ * that is cut into parts, the parts are held to 2^-39 of the largest magnitude in their row's head: a column that much smaller than another
+ * comes out as 0.  A value of a bf16 pool that is not finite may reach every row of its step, also those that do
  * not see its position (0 * NaN); the 8-bit format keeps it from them. */
 arb_status arb_stage_attention_kv(const arb_model *m, const void *q, int32_t q_row_stride, int32_t q_scaled,
                                   const arb_kv_layer *kv, float softcap, const arb_batch *batch, void *out, void *ws,

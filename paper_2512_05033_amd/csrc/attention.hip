@@ -4,7 +4,7 @@
 // that share hk and the s_b step tokens form s_b*G query rows (row = i*G + g,
 // token-major).  A workgroup of 4 waves takes 128 rows (32 per wave) and one
 // chunk of the key range ("split"); chunks of a sequence are merged afterwards
-// from their online-softmax states (m, l) and normalised partial results (bf16).  Every KV byte is
+// from their online-softmax states (m, l) and normalised partial results (16 bits).  Every KV byte is
 // streamed from HBM once per 128 rows that need it; rows of different query
 // tiles of the same (b, hk) meet in L2.
 //
@@ -492,8 +492,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(
   if (!wave_active) return;
   // With SPLIT this is the split's own normalised result (it lies in the hull of the values, like the output) in 16 bits plus its
   // (m, l) in fp32: half the partial traffic of fp32 accumulators.  bf16 over an uncapped bf16 cache, as ever; otherwise fp16
-  // relative to a power of two that puts the row's largest at 2^14, with three bits more (error against 64 bits, 16 steps of 64 in five
-  // parts: 0.0023 of the result's norm in bf16, 0.0017 this way, 0.0016 with one rounding, the result's).
+  // relative to a power of two that puts the row's largest at 2^14: three bits more (error against 64 bits, 16 steps of 64 in five
+  // parts: 0.0023 of the result's norm in bf16, 0.0017 this way, 0.0016 with one rounding, the result's) down to 2^-28 of that
+  // largest, and a multiple of 2^-39 of it below, where bf16 would keep the precision of each column.
   constexpr bool RELATIVE = SPLIT && (KV8 || CAP);
   const float inv = !SPLIT || l_tot > 0.f ? 1.0f / l_tot : 0.f;
   float scale = 1.f, rel = 1.f;
@@ -762,7 +763,7 @@ AttnPlan plan_attention_fine(int batch, const int32_t *prefix_host, const int32_
   return plan_of_chunk(batch, prefix_host, cu_host, G, n_kv_heads, (int)chunk, max_ctx, max_step);
 }
 
-// Workspace: partial results [splits, T, Hq, hd] bf16 and their (m, l) fp32 (none with a single split), the splits of every
+// Workspace: partial results [splits, T, Hq, hd] in 16 bits and two fp32 beside each row (none with a single split), the splits of every
 // token, the work list (none with n_items == 0).
 static size_t part_acc_bytes(int max_splits, int T, int Hq, int hd) {
   return max_splits > 1 ? align_up((size_t)max_splits * T * Hq * hd * sizeof(bf16), 256) : 0;
